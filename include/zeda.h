@@ -202,6 +202,44 @@ zeda_status_t zeda_moe_stats(zeda_moe_t *h, const void *x, int32_t T, float *f, 
  * Reads the routing kept in the workspace; computes nothing else. */
 zeda_status_t zeda_moe_token_zero_share(zeda_moe_t *h, int32_t T, float *r_ze, void *stream);
 
+/* ---- Training objective: the router's part (Section 2.2) ------------------------------------------------
+ * The load-balancing losses over a batch and the gradient to the router's logits.  p = softmax(logits) over the
+ * N+N_Z candidates; n tokens count (those whose mask is not 0); f_i = slots of those tokens on candidate i / n,
+ * P_i = mean of p_i over them; f_E, P_E are sums over the normal experts, f_Z, P_Z over the zero experts:
+ *   ZEDA_BALANCE_GROUP    L_GA = alpha (N + N_Z w)/K (f_E P_E / N + f_Z P_Z / (N_Z w))   (Eq. 5, 6; N_Z = 0: first term)
+ *   ZEDA_BALANCE_VANILLA  L_A  = alpha (N + N_Z)/K sum_i f_i P_i                         (Eq. 4; group_w is not used) */
+typedef enum { ZEDA_BALANCE_GROUP = 0, ZEDA_BALANCE_VANILLA = 1 } zeda_balance_kind_t;
+typedef struct {
+    int32_t kind;    /* zeda_balance_kind_t */
+    float alpha;     /* finite */
+    float group_w;   /* w: positive and finite */
+} zeda_balance_t;
+
+/* The loss with its per-candidate counts, from the logits (zeda_router_logits) and the ids chosen from them.
+ *   logits     dev [T, N+N_Z] fp32        topk_idx   dev [T, K] int32 (ids outside [0, N+N_Z) count nowhere)
+ *   token_mask dev [T] uint8, 0 = the token does not count and its logits and ids are not read; NULL = all count
+ *   loss       dev [1] fp32               counts     dev [N+N_Z] int32: slots of the counting tokens
+ *   p_mean     dev [N+N_Z] fp32 = P_i, or NULL           n_tokens   dev [1] int32 = n
+ * Without a counting token everything is 0.  A token all of whose logits are -inf has p = 0; NaN propagates.
+ * Needs no weights: it uses the handle's shape and workspace, and leaves the routing kept in the handle alone.
+ * Results do not change from call to call.  T == 0 returns ZEDA_OK and touches nothing. */
+zeda_status_t zeda_moe_balance_loss(zeda_moe_t *h, const float *logits, const int32_t *topk_idx, const uint8_t *token_mask, int32_t T,
+                                    const zeda_balance_t *balance, float *loss, int32_t *counts, float *p_mean, int32_t *n_tokens,
+                                    void *stream);
+
+/* The gradient to the logits, in one pass: that of the balance loss (grad_loss given) plus that of the routing weights
+ * of the handle's gate_mode (grad_topk_w given); one of the two at least.
+ *   counts, n_tokens  dev, as zeda_moe_balance_loss wrote them; sums of several calls' (or ranks') counts and tokens give
+ *                     the gradient of the loss over all of them.  Read with grad_loss only; constants, as the counts are
+ *   grad_loss    dev [1] fp32 gradient of the loss value, or NULL (then balance, counts and n_tokens may be NULL)
+ *   grad_topk_w  dev [T, K] fp32 gradient of topk_w (zeda_route), or NULL (then topk_idx may be NULL).  Slots whose id
+ *                lies outside [0, N+N_Z) are no slots; an id that comes twice in a token gets both slots' gradients
+ *   grad_logits  dev [T, N+N_Z] fp32, fully overwritten; tokens whose mask is 0 get zeros; must not overlap logits
+ * T == 0 returns ZEDA_OK and touches nothing. */
+zeda_status_t zeda_moe_router_backward(zeda_moe_t *h, const float *logits, const int32_t *topk_idx, const uint8_t *token_mask, int32_t T,
+                                       const zeda_balance_t *balance, const int32_t *counts, const int32_t *n_tokens,
+                                       const float *grad_loss, const float *grad_topk_w, float *grad_logits, void *stream);
+
 /* Counters of the last forward call, read back after synchronising the stream (blocking):
  * out[0] = P (surviving pairs), out[1] = U (normal experts with at least one pair),
  * out[2] = zero-expert slots, out[3] = kernels launched by that call. */

@@ -1,0 +1,457 @@
+// The load-balancing losses of a router with their counts (Section 2.2, Eq. 4-6), and the gradient that reaches its
+// logits: from those losses and from the routing weights.
+//
+//   p_t = softmax(l_t) over the N + N_Z candidates, n tokens that count, c_i slots of theirs on candidate i,
+//   f_i = c_i / n,  P_i = 1/n sum_t p_ti
+//   L_A  = alpha (N + N_Z) / K sum_i f_i P_i                                                         (Eq. 4)
+//   L_GA = alpha (N + N_Z w) / K (f_E P_E / N + f_Z P_Z / (N_Z w)),  f_E, P_E sums over the normal
+//          experts, f_Z, P_Z over the zero experts                                                   (Eq. 5, 6)
+// The counts have no gradient.  Both losses are sum_i s_i P_i with slopes s that depend on the counts alone, so
+//   dL/dl_ti = 1/n p_ti (s_i - sum_j p_tj s_j).
+// A routing weight is a softmax too, of the chosen candidates' logits (or of all: GATE_SOFTMAX_RAW), with the same form
+// of derivative; both gradients end in the same T x (N + N_Z) numbers and are written by one pass.
+//
+// One warp per token, candidate j in lane j % 32, register j / 32, fp32 throughout.  What bounds both kernels is the
+// logits' way through HBM (the losses read them once, the gradient reads and writes them once); small calls are latency.
+#include <cooperative_groups.h>
+
+#include "route_token.cuh"
+
+namespace zeda {
+
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kLossWarps = 16;               // of a CTA of the loss kernel
+constexpr int kLossThreads = 32 * kLossWarps;
+constexpr int kLossCluster = 8;              // CTAs that add up their sums among themselves first
+constexpr int kLossMaxCtas = 144;            // 18 clusters of 8: one CTA per SM
+constexpr int kGradWarps = 8;
+
+// What the losses' slopes are made of, as the kernels take it.
+struct BalanceArgs {
+    int kind, n_real, n_cand, K;
+    float alpha, group_w;
+};
+
+template <int RPL>
+__device__ __forceinline__ void load_logits(const float *__restrict__ row, int n_cand, int lane, float (&v)[RPL]) {
+#pragma unroll
+    for (int r = 0; r < RPL; ++r) v[r] = ldcg_if(r * 32 + lane < n_cand, row + r * 32 + lane, -INFINITY);
+}
+
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, o));
+    return v;
+}
+
+// Softmax of one token in place, p = expf(l - m) * inv.  A token all of whose logits are -inf has probabilities 0; a NaN
+// stays one.
+template <int RPL>
+__device__ __forceinline__ void softmax_row(float (&v)[RPL], float &m, float &inv) {
+    m = v[0];
+#pragma unroll
+    for (int r = 1; r < RPL; ++r) m = fmaxf(m, v[r]);
+    m = warp_max(m);
+    if (m == -INFINITY) m = 0.f;
+    float sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < RPL; ++r) {
+        v[r] = expf(v[r] - m);
+        sum += v[r];
+    }
+    sum = warp_sum(sum);
+    inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int r = 0; r < RPL; ++r) v[r] *= inv;
+}
+
+// Sums over the tokens: probabilities and counts per candidate, tokens that count.  Every warp adds up its tokens in
+// registers, the warps of a CTA through shared memory, the CTAs of a cluster through each other's, each taking a share of
+// the columns; the clusters' sums go to the workspace, and the CTA that finishes last adds those and writes the results.
+// The order of every sum is fixed by T alone.
+template <int RPL>
+__global__ void __launch_bounds__(kLossThreads, 1)
+balance_loss_kernel(const float *__restrict__ logits, const int32_t *__restrict__ topk_idx, const uint8_t *__restrict__ mask, int T,
+                    const BalanceArgs a, float *__restrict__ part, int32_t *__restrict__ part_counts, int32_t *__restrict__ done,
+                    float *__restrict__ loss, int32_t *__restrict__ counts, float *__restrict__ p_mean,
+                    int32_t *__restrict__ n_tokens) {
+    pdl_launch_dependents();
+    extern __shared__ float warp_cols[];  // [kLossWarps][n_cand]
+    __shared__ float col[kMaxCand];
+    __shared__ int32_t hist[kMaxCand + 1];  // the last: tokens
+    __shared__ double red[4][kLossWarps];
+    __shared__ int s_last;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int C = a.n_cand;
+    for (int i = threadIdx.x; i <= kMaxCand; i += kLossThreads) hist[i] = 0;
+    __syncthreads();
+    pdl_wait();
+
+    float acc[RPL];
+#pragma unroll
+    for (int r = 0; r < RPL; ++r) acc[r] = 0.f;
+    int my_tokens = 0;
+    const int stride = gridDim.x * kLossWarps;
+    const int first = blockIdx.x + warp * gridDim.x;  // consecutive tokens to different SMs
+    for (int t = first; t < T; t += 2 * stride) {
+        float v[2][RPL];
+        bool on[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int tt = t + n * stride;
+            on[n] = tt < T && (!mask || __ldcg(mask + tt) != 0);
+            if (on[n]) {
+                load_logits<RPL>(logits + (size_t)tt * C, C, lane, v[n]);
+                if (lane < a.K) {
+                    const int id = __ldcg(topk_idx + (size_t)tt * a.K + lane);
+                    if (id >= 0 && id < C) atomicAdd(&hist[id], 1);
+                }
+                ++my_tokens;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+            if (on[n]) {
+                float m, inv;
+                softmax_row<RPL>(v[n], m, inv);
+#pragma unroll
+                for (int r = 0; r < RPL; ++r) acc[r] += v[n][r];
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < RPL; ++r)
+        if (r * 32 + lane < C) warp_cols[warp * C + r * 32 + lane] = acc[r];
+    if (lane == 0) atomicAdd(&hist[kMaxCand], my_tokens);
+    __syncthreads();
+    for (int j = threadIdx.x; j < C; j += kLossThreads) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < kLossWarps; ++w) s += warp_cols[w * C + j];
+        col[j] = s;
+    }
+    cg::cluster_group cluster = cg::this_cluster();
+    const int cs = cluster.num_blocks(), cr = cluster.block_rank();
+    const int n_clusters = gridDim.x / cs, cid = blockIdx.x / cs;
+    cluster.sync();
+    // columns 0..C-1, and C for the tokens
+    for (int j = cr * kLossThreads + threadIdx.x; j <= C; j += cs * kLossThreads) {
+        float s = 0.f;
+        int n = 0;
+        const int h = j < C ? j : kMaxCand;
+        for (int r = 0; r < cs; ++r) {
+            if (j < C) s += *cluster.map_shared_rank(&col[j], r);
+            n += *cluster.map_shared_rank(&hist[h], r);
+        }
+        if (j < C) part[(size_t)cid * C + j] = s;
+        part_counts[(size_t)cid * (C + 1) + j] = n;
+    }
+    cluster.sync();  // no CTA leaves while another reads its sums; also the stores above come before the count below
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) s_last = atomicInc(reinterpret_cast<unsigned *>(done), gridDim.x - 1) == gridDim.x - 1;  // back at 0 behind the last
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+
+    int n = 0;
+    for (int c = 0; c < n_clusters; ++c) n += __ldcg(part_counts + (size_t)c * (C + 1) + C);
+    const double inv_n = n > 0 ? 1.0 / (double)n : 0.0;
+    double s4[4] = {0.0, 0.0, 0.0, 0.0};  // vanilla: sum f_i P_i; group: f_E, P_E, and f_Z, P_Z
+    for (int j = threadIdx.x; j < C; j += kLossThreads) {
+        float s = 0.f;
+        int k = 0;
+        for (int c = 0; c < n_clusters; ++c) {
+            s += __ldcg(part + (size_t)c * C + j);
+            k += __ldcg(part_counts + (size_t)c * (C + 1) + j);
+        }
+        const double f = k * inv_n, P = n > 0 ? s * inv_n : 0.0;
+        counts[j] = k;
+        if (p_mean) p_mean[j] = (float)P;
+        if (a.kind == ZEDA_BALANCE_VANILLA) s4[0] += f * P;
+        else if (j < a.n_real) { s4[0] += f; s4[1] += P; }
+        else { s4[2] += f; s4[3] += P; }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s4[i] += __shfl_xor_sync(kFull, s4[i], o);
+        if (lane == 0) red[i][warp] = s4[i];
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double t4[4];
+        for (int i = 0; i < 4; ++i) {
+            t4[i] = 0.0;
+            for (int w = 0; w < kLossWarps; ++w) t4[i] += red[i][w];
+        }
+        const int Z = C - a.n_real;
+        double L;
+        if (a.kind == ZEDA_BALANCE_VANILLA) {
+            L = (double)a.alpha * C / a.K * t4[0];
+        } else {
+            L = t4[0] * t4[1] / a.n_real;
+            if (Z > 0) L += t4[2] * t4[3] / ((double)Z * a.group_w);
+            L *= (double)a.alpha * (a.n_real + (double)Z * a.group_w) / a.K;
+        }
+        *loss = (float)L;
+        *n_tokens = n;
+    }
+}
+
+// Gradient to the logits.  The slopes are taken relative to candidate 0's (the softmax's derivative does not see a
+// constant), so that a group's common slope, or the mean load, costs no digits of the differences that are left.
+template <int RPL>
+__global__ void __launch_bounds__(32 * kGradWarps)
+router_backward_kernel(const float *__restrict__ logits, const int32_t *__restrict__ topk_idx, const uint8_t *__restrict__ mask, int T,
+                       const BalanceArgs a, int gate_mode, const int32_t *__restrict__ counts, const int32_t *__restrict__ n_tokens,
+                       const float *__restrict__ grad_loss, const float *__restrict__ grad_topk_w, float *__restrict__ grad_logits) {
+    pdl_launch_dependents();
+    extern __shared__ float slot_rows[];  // [kGradWarps][n_cand]: what the chosen candidates get from the routing weights
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int C = a.n_cand, K = a.K;
+    float *slots = slot_rows + warp * C;
+    for (int j = lane; j < C; j += 32) slots[j] = 0.f;
+    pdl_wait();
+
+    float slope[RPL];
+#pragma unroll
+    for (int r = 0; r < RPL; ++r) slope[r] = 0.f;
+    if (grad_loss) {
+        const double n = max(__ldcg(n_tokens), 1);
+        const double scale = (double)__ldcg(grad_loss) * a.alpha / a.K / (n * n);
+        if (a.kind == ZEDA_BALANCE_VANILLA) {
+            const int c0 = __ldcg(counts);
+            const float per = (float)(scale * C);
+#pragma unroll
+            for (int r = 0; r < RPL; ++r)
+                if (r * 32 + lane < C) slope[r] = per * (float)(__ldcg(counts + r * 32 + lane) - c0);
+        } else if (C > a.n_real) {
+            long long cE = 0, cZ = 0;
+#pragma unroll
+            for (int r = 0; r < RPL; ++r) {
+                const int j = r * 32 + lane;
+                const int c = j < C ? __ldcg(counts + j) : 0;
+                if (j < a.n_real) cE += c;
+                else cZ += c;
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                cE += __shfl_xor_sync(kFull, cE, o);
+                cZ += __shfl_xor_sync(kFull, cZ, o);
+            }
+            const double Z = C - a.n_real, w = a.group_w;
+            const float step = (float)(scale * (a.n_real + Z * w) * ((double)cZ / (Z * w) - (double)cE / a.n_real));
+#pragma unroll
+            for (int r = 0; r < RPL; ++r) slope[r] = r * 32 + lane >= a.n_real ? step : 0.f;
+        }  // (without zero experts every slope is the same)
+    }
+
+    for (int t = blockIdx.x + warp * gridDim.x; t < T; t += gridDim.x * kGradWarps) {
+        float *out = grad_logits + (size_t)t * C;
+        if (mask && __ldcg(mask + t) == 0) {
+#pragma unroll
+            for (int r = 0; r < RPL; ++r)
+                if (r * 32 + lane < C) out[r * 32 + lane] = 0.f;
+            continue;
+        }
+        const float *row = logits + (size_t)t * C;
+        float p[RPL];
+        load_logits<RPL>(row, C, lane, p);
+        int id = -1;
+        float g = 0.f, lk = -INFINITY;
+        if (grad_topk_w && lane < K) {
+            id = __ldcg(topk_idx + (size_t)t * K + lane);
+            if (id < 0 || id >= C || (gate_mode == ZEDA_GATE_RENORM_REAL && id >= a.n_real)) id = -1;
+            if (id >= 0) {
+                g = __ldcg(grad_topk_w + (size_t)t * K + lane);
+                lk = __ldcg(row + id);
+            }
+        }
+        float m, inv;
+        softmax_row<RPL>(p, m, inv);
+        float all = 0.f;  // sum_j p_j s_j
+        if (grad_loss) {
+#pragma unroll
+            for (int r = 0; r < RPL; ++r) all += r * 32 + lane < C ? p[r] * slope[r] : 0.f;
+            all = warp_sum(all);
+        }
+        float raw = 0.f;  // raw softmax: sum over the slots of p_k g_k, which every candidate feels
+        if (grad_topk_w) {
+            // the slots' weights: softmax over the chosen logits, or the chosen entries of the softmax over all
+            float u;
+            if (gate_mode == ZEDA_GATE_SOFTMAX_RAW) {
+                u = id >= 0 ? expf(lk - m) * inv * g : 0.f;
+                raw = warp_sum(u);
+            } else {
+                float mk = warp_max(lk);
+                if (mk == -INFINITY) mk = 0.f;
+                const float e = id >= 0 ? expf(lk - mk) : 0.f;
+                const float sum = warp_sum(e);
+                const float w = sum == 0.f ? 0.f : e / sum;
+                u = w * (g - warp_sum(w * g));
+            }
+            // one slot after the other, each by the lane that owns its column: an id that comes twice gets both
+            for (int k = 0; k < K; ++k) {
+                const int idk = __shfl_sync(kFull, id, k);
+                const float uk = __shfl_sync(kFull, u, k);
+                if (idk >= 0 && lane == (idk & 31)) slots[idk] += uk;
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < RPL; ++r) {
+            const int j = r * 32 + lane;
+            if (j < C) {
+                float d = p[r] * (slope[r] - all - raw);
+                if (grad_topk_w) {
+                    d += slots[j];
+                    slots[j] = 0.f;
+                }
+                out[j] = d;
+            }
+        }
+    }
+}
+
+bool balance_ok(const zeda_balance_t *b) {
+    const char *why = nullptr;
+    if (!b) why = "the balance loss's description is NULL";
+    else if (b->kind != ZEDA_BALANCE_GROUP && b->kind != ZEDA_BALANCE_VANILLA) why = "unknown kind of balance loss";
+    else if (!(b->alpha - b->alpha == 0.f)) why = "alpha must be finite";
+    else if (!(b->group_w > 0.f) || !(b->group_w - b->group_w == 0.f)) why = "group_w must be positive and finite";
+    if (why) set_error("%s", why);
+    return why == nullptr;
+}
+
+bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+BalanceArgs balance_args(const zeda_moe *h, const zeda_balance_t *b) {
+    const zeda_moe_config_t &c = h->cfg;
+    BalanceArgs a = {ZEDA_BALANCE_GROUP, c.n_real, c.n_real + c.n_zero, c.top_k, 0.f, 1.f};
+    if (b) { a.kind = b->kind; a.alpha = b->alpha; a.group_w = b->group_w; }
+    return a;
+}
+
+zeda_status_t loss_call_ok(zeda_moe *h, int T) {
+    if (!h) { set_error("handle is NULL"); return ZEDA_ERR_INVALID_ARG; }
+    if (T < 0 || T > h->cfg.max_tokens) { set_error("T=%d outside [0, max_tokens=%d]", T, h->cfg.max_tokens); return ZEDA_ERR_INVALID_ARG; }
+    return ZEDA_OK;
+}
+
+zeda_status_t on_device(zeda_moe *h) {
+    const cudaError_t e = cudaSetDevice(h->cfg.device);
+    if (e == cudaSuccess) return ZEDA_OK;
+    set_error("cudaSetDevice: %s", cudaGetErrorString(e));
+    return ZEDA_ERR_CUDA;
+}
+
+template <int RPL>
+cudaError_t launch_balance(const zeda_moe *h, const float *logits, const int32_t *topk_idx, const uint8_t *mask, int T,
+                           const BalanceArgs &a, float *loss, int32_t *counts, float *p_mean, int32_t *n_tokens, cudaStream_t s) {
+    // a CTA for 32 tokens, in whole clusters
+    int ctas = (T + 2 * kLossWarps - 1) / (2 * kLossWarps);
+    if (ctas > kLossMaxCtas) ctas = kLossMaxCtas;
+    int cs = kLossCluster;
+    while (cs > ctas) cs /= 2;
+    ctas = ctas / cs * cs;
+    const int max_clusters = kLossMaxCtas / kLossCluster;
+    float *part = h->ws.stat_part;
+    int32_t *part_counts = reinterpret_cast<int32_t *>(part + (size_t)max_clusters * a.n_cand);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(kLossThreads);
+    cfg.dynamicSmemBytes = (size_t)kLossWarps * a.n_cand * sizeof(float);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cs;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = h->pdl ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, balance_loss_kernel<RPL>, logits, topk_idx, mask, T, a, part, part_counts,
+                              h->ws.meta + kMetaBalanceDone, loss, counts, p_mean, n_tokens);
+}
+
+template <int RPL>
+cudaError_t launch_backward(const zeda_moe *h, const float *logits, const int32_t *topk_idx, const uint8_t *mask, int T,
+                            const BalanceArgs &a, const int32_t *counts, const int32_t *n_tokens, const float *grad_loss,
+                            const float *grad_topk_w, float *grad_logits, cudaStream_t s) {
+    int ctas = (T + kGradWarps - 1) / kGradWarps;
+    const int most = h->sm_count * 4;
+    if (ctas > most) ctas = most;
+    return launch_kernel(h->pdl, router_backward_kernel<RPL>, dim3(ctas), dim3(32 * kGradWarps),
+                         (size_t)kGradWarps * a.n_cand * sizeof(float), s, logits, topk_idx, mask, T, a, (int)h->cfg.gate_mode, counts,
+                         n_tokens, grad_loss, grad_topk_w, grad_logits);
+}
+
+}  // namespace
+
+#define ZEDA_LOSS_DISPATCH(CALL, ...)                   \
+    (a.n_cand <= 32    ? CALL<1>(__VA_ARGS__)           \
+     : a.n_cand <= 64  ? CALL<2>(__VA_ARGS__)           \
+     : a.n_cand <= 96  ? CALL<3>(__VA_ARGS__)           \
+     : a.n_cand <= 128 ? CALL<4>(__VA_ARGS__)           \
+     : a.n_cand <= 192 ? CALL<6>(__VA_ARGS__)           \
+     : a.n_cand <= 256 ? CALL<8>(__VA_ARGS__)           \
+                       : CALL<16>(__VA_ARGS__))
+
+}  // namespace zeda
+
+using namespace zeda;
+
+extern "C" zeda_status_t zeda_moe_balance_loss(zeda_moe_t *h, const float *logits, const int32_t *topk_idx, const uint8_t *token_mask,
+                                               int32_t T, const zeda_balance_t *balance, float *loss, int32_t *counts, float *p_mean,
+                                               int32_t *n_tokens, void *stream) {
+    zeda_status_t st = loss_call_ok(h, T);
+    if (st != ZEDA_OK || T == 0) return st;
+    if (!balance_ok(balance)) return ZEDA_ERR_INVALID_ARG;
+    if (!logits || !topk_idx || !loss || !counts || !n_tokens) {
+        set_error("logits, topk_idx, loss, counts and n_tokens are required");
+        return ZEDA_ERR_INVALID_ARG;
+    }
+    if (!aligned4(logits) || !aligned4(topk_idx) || !aligned4(loss) || !aligned4(counts) || !aligned4(p_mean) || !aligned4(n_tokens)) {
+        set_error("fp32 and int32 arrays must be 4-byte aligned");
+        return ZEDA_ERR_INVALID_ARG;
+    }
+    if ((st = on_device(h)) != ZEDA_OK) return st;
+    const BalanceArgs a = balance_args(h, balance);
+    const cudaError_t e = ZEDA_LOSS_DISPATCH(launch_balance, h, logits, topk_idx, token_mask, T, a, loss, counts, p_mean, n_tokens,
+                                             static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) { set_error("balance loss launch: %s", cudaGetErrorString(e)); return ZEDA_ERR_CUDA; }
+    h->last_launches = 1;
+    return ZEDA_OK;
+}
+
+extern "C" zeda_status_t zeda_moe_router_backward(zeda_moe_t *h, const float *logits, const int32_t *topk_idx, const uint8_t *token_mask,
+                                                  int32_t T, const zeda_balance_t *balance, const int32_t *counts,
+                                                  const int32_t *n_tokens, const float *grad_loss, const float *grad_topk_w,
+                                                  float *grad_logits, void *stream) {
+    zeda_status_t st = loss_call_ok(h, T);
+    if (st != ZEDA_OK || T == 0) return st;
+    if (!grad_loss && !grad_topk_w) { set_error("grad_loss and grad_topk_w are both NULL"); return ZEDA_ERR_INVALID_ARG; }
+    if (grad_loss) {
+        if (!balance_ok(balance)) return ZEDA_ERR_INVALID_ARG;
+        if (!counts || !n_tokens) { set_error("the balance loss's gradient needs counts and n_tokens"); return ZEDA_ERR_INVALID_ARG; }
+    }
+    if (!logits || !grad_logits) { set_error("logits and grad_logits are required"); return ZEDA_ERR_INVALID_ARG; }
+    if (grad_topk_w && !topk_idx) { set_error("the routing weights' gradient needs topk_idx"); return ZEDA_ERR_INVALID_ARG; }
+    if (!aligned4(logits) || !aligned4(topk_idx) || !aligned4(counts) || !aligned4(n_tokens) || !aligned4(grad_loss) ||
+        !aligned4(grad_topk_w) || !aligned4(grad_logits)) {
+        set_error("fp32 and int32 arrays must be 4-byte aligned");
+        return ZEDA_ERR_INVALID_ARG;
+    }
+    const BalanceArgs a = balance_args(h, grad_loss ? balance : nullptr);
+    const size_t bytes = (size_t)T * a.n_cand * sizeof(float);
+    const char *lb = reinterpret_cast<const char *>(logits), *gb = reinterpret_cast<const char *>(grad_logits);
+    if (lb < gb + bytes && gb < lb + bytes) { set_error("logits and grad_logits overlap"); return ZEDA_ERR_INVALID_ARG; }
+    if ((st = on_device(h)) != ZEDA_OK) return st;
+    const cudaError_t e = ZEDA_LOSS_DISPATCH(launch_backward, h, logits, topk_idx, token_mask, T, a, counts, n_tokens, grad_loss,
+                                             grad_topk_w, grad_logits, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) { set_error("router backward launch: %s", cudaGetErrorString(e)); return ZEDA_ERR_CUDA; }
+    h->last_launches = 1;
+    return ZEDA_OK;
+}

@@ -38,6 +38,7 @@ enum MetaSlot {
     kMetaNextItem1 = 8,  // next unclaimed work item of the GEMM1 kernel (reset by the routing pass)
     kMetaNextItem2 = 9,  // the same for GEMM2
     kMetaRouted = 10,    // smallest batches: the routing tables of the call are in the workspace (the router clears it)
+    kMetaBalanceDone = 11, // CTAs of a balance-loss call that are done (the last sets it back to 0)
     kMetaCount = 16
 };
 

@@ -19,12 +19,13 @@ STAGES = ("router", "sort", "gemm1", "gemm2", "combine")
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = 0, -1, -2, -3, -4, -5
 GATE_TOPK_NORM, GATE_SOFTMAX_RAW, GATE_RENORM_REAL = 0, 1, 2
 EXPERT_ZERO, EXPERT_COPY = 0, 1
+BALANCE_GROUP, BALANCE_VANILLA = 0, 1
 FLAG_NONE, FLAG_NO_DEPENDENT_LAUNCH = 0, 4
 
 EXPORTS = (
     "zeda_moe_workspace_bytes", "zeda_moe_create", "zeda_route", "zeda_route_from_logits",
     "zeda_router_logits", "zeda_moe_forward", "zeda_moe_forward_residual", "zeda_moe_forward_host", "zeda_moe_stats",
-    "zeda_moe_token_zero_share", "zeda_moe_last_counters", "zeda_moe_set_profiling", "zeda_moe_stage_ms", "zeda_residual_rmsnorm",
+    "zeda_moe_balance_loss", "zeda_moe_router_backward", "zeda_moe_token_zero_share", "zeda_moe_last_counters", "zeda_moe_set_profiling", "zeda_moe_stage_ms", "zeda_residual_rmsnorm",
     "zeda_moe_selftest_wait", "zeda_moe_clear_error",
     "zeda_ep_dispatch", "zeda_ep_experts", "zeda_ep_combine",
     "zeda_compact_static", "zeda_moe_destroy", "zeda_last_error", "zeda_version",
@@ -35,6 +36,10 @@ class Config(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "d_model", "d_expert", "n_real", "n_zero", "top_k", "max_tokens", "gate_mode", "expert_kind",
         "device", "flags", "ep_size", "ep_rank", "max_recv_pairs")]
+
+
+class Balance(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("alpha", ctypes.c_float), ("group_w", ctypes.c_float)]
 
 
 class ZedaError(RuntimeError):
@@ -68,6 +73,10 @@ def _load() -> ctypes.CDLL:
     lib.zeda_moe_stats.argtypes = [vp, vp, i32, vp, vp, vp, vp]
     lib.zeda_moe_token_zero_share.restype = i32
     lib.zeda_moe_token_zero_share.argtypes = [vp, i32, vp, vp]
+    lib.zeda_moe_balance_loss.restype = i32
+    lib.zeda_moe_balance_loss.argtypes = [vp, vp, vp, vp, i32, ctypes.POINTER(Balance), vp, vp, vp, vp, vp]
+    lib.zeda_moe_router_backward.restype = i32
+    lib.zeda_moe_router_backward.argtypes = [vp, vp, vp, vp, i32, ctypes.POINTER(Balance), vp, vp, vp, vp, vp, vp]
     lib.zeda_moe_last_counters.restype = i32
     lib.zeda_moe_last_counters.argtypes = [vp, ctypes.POINTER(ctypes.c_int64), vp]
     lib.zeda_moe_set_profiling.restype = i32
@@ -310,6 +319,55 @@ class ZedaMoE:
         the last routing call on this handle."""
         out = torch.empty(T, dtype=torch.float32, device=self.device)
         _check(lib.zeda_moe_token_zero_share(self._h, T, _ptr(out), _stream(self.device)))
+        return out
+
+    # -- training objective --------------------------------------------------------------------
+    def _check_loss_inputs(self, logits, topk_idx, token_mask) -> int:
+        assert logits.device == self.device and logits.dtype == torch.float32 and logits.is_contiguous()
+        assert logits.dim() == 2 and logits.shape[1] == self.E + self.Z
+        T = logits.shape[0]
+        if topk_idx is not None:
+            assert topk_idx.device == self.device and topk_idx.dtype == torch.int32 and topk_idx.is_contiguous()
+            assert topk_idx.shape == (T, self.K)
+        if token_mask is not None:
+            assert token_mask.device == self.device and token_mask.dtype in (torch.uint8, torch.bool)
+            assert token_mask.is_contiguous() and token_mask.shape == (T,)
+        return T
+
+    def balance_loss(self, logits: torch.Tensor, topk_idx: torch.Tensor, alpha: float, group_w: float = 1.0,
+                     kind: int = BALANCE_GROUP, token_mask: Optional[torch.Tensor] = None):
+        """zeda_moe_balance_loss: (loss [1], counts [N+N_Z], p_mean [N+N_Z], n_tokens [1]) of the batch's router
+        logits and chosen ids; asynchronous on the current stream.  Without tokens everything is 0."""
+        T = self._check_loss_inputs(logits, topk_idx, token_mask)
+        n, dev = self.E + self.Z, self.device
+        new = torch.empty if T else torch.zeros
+        loss = new(1, dtype=torch.float32, device=dev)
+        counts = new(n, dtype=torch.int32, device=dev)
+        p_mean = new(n, dtype=torch.float32, device=dev)
+        n_tokens = new(1, dtype=torch.int32, device=dev)
+        b = Balance(int(kind), float(alpha), float(group_w))
+        _check(lib.zeda_moe_balance_loss(self._h, _ptr(logits), _ptr(topk_idx), _ptr(token_mask), T, ctypes.byref(b), _ptr(loss),
+                                         _ptr(counts), _ptr(p_mean), _ptr(n_tokens), _stream(dev)))
+        return loss, counts, p_mean, n_tokens
+
+    def router_backward(self, logits: torch.Tensor, topk_idx: Optional[torch.Tensor] = None,
+                        grad_topk_w: Optional[torch.Tensor] = None, grad_loss: Optional[torch.Tensor] = None,
+                        counts: Optional[torch.Tensor] = None, n_tokens: Optional[torch.Tensor] = None, alpha: float = 0.0,
+                        group_w: float = 1.0, kind: int = BALANCE_GROUP, token_mask: Optional[torch.Tensor] = None,
+                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """zeda_moe_router_backward: gradient [T, N+N_Z] to the logits from the routing weights' (grad_topk_w, with
+        topk_idx) and from the balance loss's (grad_loss [1], with counts and n_tokens of balance_loss, alpha, group_w
+        and kind as there); asynchronous on the current stream."""
+        T = self._check_loss_inputs(logits, topk_idx, token_mask)
+        for t, dtype, shape in ((grad_topk_w, torch.float32, (T, self.K)), (grad_loss, torch.float32, (1,)),
+                                (counts, torch.int32, (self.E + self.Z,)), (n_tokens, torch.int32, (1,)),
+                                (out, torch.float32, tuple(logits.shape))):
+            assert t is None or (t.device == self.device and t.dtype == dtype and t.is_contiguous() and t.shape == shape)
+        if out is None:
+            out = torch.empty_like(logits)
+        b = Balance(int(kind), float(alpha), float(group_w))
+        _check(lib.zeda_moe_router_backward(self._h, _ptr(logits), _ptr(topk_idx), _ptr(token_mask), T, ctypes.byref(b), _ptr(counts),
+                                            _ptr(n_tokens), _ptr(grad_loss), _ptr(grad_topk_w), _ptr(out), _stream(self.device)))
         return out
 
     def last_counters(self):

@@ -342,6 +342,55 @@ zeda_status_t zeda_ep_combine(zeda_moe_t *h, const void *x, const void *back_row
 zeda_status_t zeda_moe_selftest_wait(zeda_moe_t *h, int32_t limit_us, void *stream);
 zeda_status_t zeda_moe_clear_error(zeda_moe_t *h, void *stream);
 
+/* ---- Training objective: the token term (Eq. 2; weighted token by token, Eq. 3) -----------------------
+ * Negative log likelihood of given tokens under a vocabulary matrix, nll_t = log sum_v exp(<x_t, w_v>) - <x_t, w_target>,
+ * and its gradients, without the T x n_vocab logits in memory.  fp32 sums over exact bf16 products. */
+typedef struct zeda_vocab zeda_vocab_t; /* opaque; host memory owned by the library */
+
+/* Supported: d_model a multiple of 64 in [64, 8192], 1 <= n_vocab <= 2^24, 1 <= max_tokens <= 2^20. */
+typedef struct {
+    int32_t d_model;
+    int32_t n_vocab;
+    int32_t max_tokens;  /* largest T any call will pass */
+    int32_t backward;    /* 1: zeda_vocab_nll_backward will be called (its workspace: up to 256 MB for the gradient of
+                            a piece of the logits, and 4 bytes per element of x) */
+    int32_t device;      /* CUDA device ordinal */
+    int32_t flags;       /* ZEDA_FLAG_* */
+} zeda_vocab_config_t;
+
+/* Device workspace (bytes, multiple of 256); 0 if the configuration is invalid. */
+size_t zeda_vocab_workspace_bytes(const zeda_vocab_config_t *cfg);
+
+/*   w          dev [n_vocab, d_model] bf16, 16-byte aligned; the caller keeps it alive.  Its values may change between
+ *              calls (an optimiser step): nothing is derived from them here
+ *   workspace  dev, >= zeda_vocab_workspace_bytes(cfg), 256-byte aligned
+ * Makes the configured device current and synchronises before returning.  A handle's calls share its workspace: they are
+ * for one stream at a time (this holds for captured graphs that are replayed, too). */
+zeda_status_t zeda_vocab_create(const zeda_vocab_config_t *cfg, const void *w, void *workspace, size_t workspace_bytes,
+                                zeda_vocab_t **out);
+
+/*   x       dev [T, d_model] bf16
+ *   target  dev [T] int32; a token whose target lies outside [0, n_vocab) carries no loss: its x is not read into any
+ *           result, its nll and lse are 0
+ *   nll     dev [T] fp32                lse  dev [T] fp32: log sum_v exp(<x_t, w_v>)
+ * T == 0 returns ZEDA_OK and touches nothing. */
+zeda_status_t zeda_vocab_nll(zeda_vocab_t *h, const void *x, const int32_t *target, int32_t T, float *nll, float *lse, void *stream);
+
+/* Gradients of sum_t grad_nll_t nll_t.  x, w and target as they were in zeda_vocab_nll, nll and lse what it wrote.
+ *   grad_nll  dev [T] fp32 (1/n for a mean over n tokens; a reward or an advantage)
+ *   grad_x    dev [T, d_model] bf16, fully overwritten; zeros for tokens without loss
+ *   grad_w    dev [n_vocab, d_model] bf16, fully overwritten
+ * grad_x and grad_w overlap nothing else.  The gradient of a logit is rounded to bf16 before the products with w and x.
+ * Results do not change from call to call.  T == 0 sets grad_w to zeros. */
+zeda_status_t zeda_vocab_nll_backward(zeda_vocab_t *h, const void *x, const int32_t *target, int32_t T, const float *nll,
+                                      const float *lse, const float *grad_nll, void *grad_x, void *grad_w, void *stream);
+
+/* Waits for the stream and reports (then clears) an expired device-side wait: ZEDA_ERR_TIMEOUT. */
+zeda_status_t zeda_vocab_check(zeda_vocab_t *h, void *stream);
+
+/* Reports a pending error word (ZEDA_ERR_TIMEOUT) if any, then releases the handle; the caller's memory is left alone. */
+zeda_status_t zeda_vocab_destroy(zeda_vocab_t *h);
+
 /* Reports a pending device-side error word (ZEDA_ERR_TIMEOUT) if any, then releases the handle.
  * Does not touch caller-owned device memory. */
 zeda_status_t zeda_moe_destroy(zeda_moe_t *h);

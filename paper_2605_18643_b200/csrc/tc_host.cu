@@ -22,11 +22,11 @@ EncodeTiledFn encode_fn() {
 }
 
 bool encode_impl(CUtensorMap *m, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides_bytes,
-                 const cuuint32_t *box) {
+                 const cuuint32_t *box, CUtensorMapDataType type) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) { set_error("cuTensorMapEncodeTiled is not available from the driver"); return false; }
     cuuint32_t ones[5] = {1, 1, 1, 1, 1};
-    CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(base), dims, strides_bytes,
+    CUresult r = fn(m, type, (cuuint32_t)rank, const_cast<void *>(base), dims, strides_bytes,
                     box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) { set_error("cuTensorMapEncodeTiled failed with code %d", (int)r); return false; }
@@ -37,7 +37,12 @@ bool encode_impl(CUtensorMap *m, const void *base, int rank, const cuuint64_t *d
 
 bool encode_bf16_map(CUtensorMap *m, const void *base, int rank, const cuuint64_t *dims,
                      const cuuint64_t *strides_bytes, const cuuint32_t *box) {
-    return encode_impl(m, base, rank, dims, strides_bytes, box);
+    return encode_impl(m, base, rank, dims, strides_bytes, box, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16);
+}
+
+bool encode_f32_map(CUtensorMap *m, const void *base, int rank, const cuuint64_t *dims,
+                    const cuuint64_t *strides_bytes, const cuuint32_t *box) {
+    return encode_impl(m, base, rank, dims, strides_bytes, box, CU_TENSOR_MAP_DATA_TYPE_FLOAT32);
 }
 
 }  // namespace zeda

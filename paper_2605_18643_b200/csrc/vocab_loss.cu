@@ -1,0 +1,946 @@
+// Negative log likelihood of given tokens under a vocabulary matrix, and its gradients, without the logits in memory: the
+// token term of the adaptation losses (Eq. 2; weighted token by token it is Eq. 3's).
+//
+//   l_tv = <x_t, w_v>,   nll_t = log sum_v exp(l_tv) - l_t,y(t)
+//   dl_tv = g_t (exp(l_tv - lse_t) - [v = y(t)]),   grad_x_t = sum_v dl_tv w_v,   grad_w_v = sum_t dl_tv x_t
+//
+// Tokens without a target are left out: the rows that carry loss are gathered to the front of a workspace first (the
+// kernels then know nothing of strides, padding or NaN in the others, and do no work for them).
+//
+// All products run on CTA pairs (tcgen05.mma.cta_group::2, 256 x 256 blocks, accumulators in TMEM, two of them, so that a
+// block's epilogue runs under the next block's products), operands by TMA:
+//   nll        X W^T; epilogue: each thread holds a token's 256 logits and leaves their maximum and sum of exponentials
+//              relative to it (8 bytes per token and 256 logits), the target's logit kept apart
+//   gradients  by pieces of the vocabulary: X W^T once more, whose epilogue writes the piece's dl as bf16, then in one
+//              launch dl W (added up in fp32 over the pieces) and dl^T X, whose operands lie with the reduction axis
+//              outermost in memory and are read in that layout (MN-major)
+// dl is rounded to bf16 because the tensor cores take both operands in one type and W and X are bf16: 2^-9 relative per
+// term, independent from term to term, so a gradient's error grows to about sqrt(2) times that of its own rounding.
+// Everything else is held in fp32.  No sum's order depends on anything but the sizes.
+#include <cstdlib>
+#include <cstring>
+#include <new>
+#include <utility>
+
+#include "tc_common.cuh"
+
+struct zeda_vocab {
+    zeda_vocab_config_t cfg;
+    bool pdl;
+    int sm_count;
+    const __nv_bfloat16 *w;
+    int rows;      // max_tokens rounded up to whole row blocks
+    int piece;     // vocabulary columns per piece of the gradient
+    int dx_rows;   // rows of the fp32 sums of grad_x
+    // workspace
+    int32_t *meta, *row_token, *row_target;
+    float *row_label, *row_lse2, *row_g, *row_gl;
+    float2 *part;
+    __nv_bfloat16 *xc, *g;
+    float *dx;
+    void *maps;    // host-side tensor maps (owned)
+};
+
+namespace zeda {
+
+namespace {
+
+using namespace tc;
+
+constexpr int kTile = 256;                       // rows and columns of a block (over the CTA pair)
+constexpr int kBlockK = 64;                      // of the reduction axis per ring stage
+constexpr int kOperandBytes = 128 * kBlockK * 2; // one CTA's half of an operand's stage
+constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kStages = 6;
+constexpr int kStoreBytes = 4096;                // an epilogue warp's patch of 32 rows x 128 bytes
+constexpr int kGemmThreads = 256;
+constexpr int kGemmSmem = kStages * kStageBytes + 8 * kStoreBytes + 1024;
+constexpr int kRowThreads = 256;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr size_t kPieceBytes = (size_t)256 << 20;  // of dl at a time
+constexpr int kMaxSplits = 16;                   // of the vocabulary axis of grad_x
+
+enum VocabMeta { kLive = 0, kVocabError = 1, kVocabMetaCount = 64 };
+
+enum { kModeNll = 0, kModeDl = 1, kModeGrads = 2 };
+
+struct VocabMaps {
+    CUtensorMap x_k, w_k, g_k;     // reduction axis innermost: [rows][k], box {64, 128}
+    CUtensorMap x_mn, w_mn, g_mn;  // reduction axis outermost: (64 elements, k, block of 64), box {64, 64, 2}
+    CUtensorMap g_store;           // [rows][piece], box {64, 32}
+    CUtensorMap dx_store;          // [dx_rows][d] fp32, box {32, 32}
+};
+
+struct GemmArgs {
+    int d, V;
+    int v0, kp;      // the piece: first vocabulary row and how many
+    int splits;      // slices of the piece that grad_x is summed in
+    int dx_pitch;    // rows between two slices' sums
+    int first;       // first piece: the sums start here
+    const int32_t *meta_live;
+    int32_t *meta;
+    const int32_t *row_target;
+    float *row_label;
+    const float *row_lse2, *row_g, *row_gl;
+    float2 *part;
+    int part_ld;
+};
+
+// A block of outputs: where its operands start and how many steps of the reduction axis it takes.
+struct Block {
+    int m, n;        // row block / column block
+    int k0, ks;      // first step and steps
+    int slice;       // grad_x: slice of the piece; -1: grad_w
+};
+
+template <int MODE>
+__device__ __forceinline__ int block_count(const GemmArgs &a, int n_rb) {
+    const int n_vt = (a.kp + kTile - 1) / kTile;
+    if (MODE != kModeGrads) return n_rb * n_vt;
+    const int dt = (a.d + kTile - 1) / kTile;
+    return (a.splits * n_rb + n_vt) * dt;
+}
+
+template <int MODE>
+__device__ __forceinline__ Block block_at(const GemmArgs &a, int i, int n_live, int n_rb) {
+    Block b;
+    if (MODE != kModeGrads) {
+        b.n = i / n_rb;
+        b.m = i % n_rb;
+        b.k0 = 0;
+        b.ks = a.d / kBlockK;
+        b.slice = 0;
+        return b;
+    }
+    const int dt = (a.d + kTile - 1) / kTile;
+    const int n_dx = a.splits * n_rb * dt;
+    if (i < n_dx) {
+        const int per = n_rb * dt;
+        b.slice = i / per;
+        b.m = (i % per) / dt;
+        b.n = i % dt;
+        const int kb = (a.kp + kBlockK - 1) / kBlockK;
+        b.k0 = (int)((long long)kb * b.slice / a.splits);
+        b.ks = (int)((long long)kb * (b.slice + 1) / a.splits) - b.k0;
+    } else {
+        const int j = i - n_dx;
+        b.slice = -1;
+        b.m = j / dt;
+        b.n = j % dt;
+        b.k0 = 0;
+        b.ks = (n_live + kBlockK - 1) / kBlockK;
+    }
+    return b;
+}
+
+// Descriptor of an MN-major bf16 tile in the 128-byte swizzle: 64 elements of the outer axis are one 128-byte row, 8 steps
+// of the reduction axis one 1024-byte group, and the next 64 elements lie 64 reduction steps further.
+__device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t addr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((addr >> 4) & 0x3fffu);
+    d |= (uint64_t)((kBlockK * 128) >> 4) << 16;  // leading byte offset: next 64 elements of the outer axis
+    d |= (uint64_t)(1024 >> 4) << 32;             // stride byte offset: next 8 steps of the reduction axis
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, int c0, int c1, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+                 ::"l"(map), "r"(c0), "r"(c1), "r"(src) : "memory");
+}
+__device__ __forceinline__ void tma_add_2d(const CUtensorMap *map, int c0, int c1, uint32_t src) {
+    asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];"
+                 ::"l"(map), "r"(c0), "r"(c1), "r"(src) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&p);
+}
+
+// One patch of 32 rows x 128 bytes to global memory: lane's row of eight 16-byte pieces into the swizzled layout, then
+// one TMA store (or addition) by one lane.  Two patches per warp: the one before is still being read.
+struct PatchWriter {
+    uint32_t base;  // of this warp's two patches
+    int lane, turn;
+    __device__ __forceinline__ uint32_t begin() {
+        if (lane == 0) bulk_wait_read<1>();
+        __syncwarp();
+        return base + (uint32_t)turn * kStoreBytes;
+    }
+    __device__ __forceinline__ void put(uint32_t patch, int piece, uint4 v) const {
+        const uint32_t at = patch + lane * 128 + ((piece ^ (lane & 7)) << 4);
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+    }
+    template <typename F>
+    __device__ __forceinline__ void end(F &&issue) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            issue();
+            bulk_commit();
+        }
+        turn ^= 1;
+    }
+};
+
+// One CTA per SM, persistent, blocks handed out in turn.  Warp 0: TMA of the A operand; warp 2: of B; warp 1: TMEM and, in
+// the leader CTA, the MMAs; warps 4-7: epilogue.  Every wait is bounded; a role that gives up records an error word and the
+// CTA leaves through the common exit.
+template <int MODE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
+vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant__ CUtensorMap map_gw, const GemmArgs a) {
+    pdl_launch_dependents();
+    extern __shared__ __align__(1024) unsigned char vocab_smem[];
+    __shared__ __align__(8) unsigned long long bars[2 * kStages + 4];
+    __shared__ uint32_t s_tmem_base;
+    __shared__ int s_abort;
+    const uint32_t ring = (smem_u32(vocab_smem) + 1023u) & ~1023u;
+    const uint32_t patches = ring + kStages * kStageBytes;
+    const uint32_t bar_full = smem_u32(&bars[0]);                 // used in the leader CTA only
+    const uint32_t bar_empty = smem_u32(&bars[kStages]);          // one set per CTA
+    const uint32_t bar_tfull = smem_u32(&bars[2 * kStages]);      // one set per CTA
+    const uint32_t bar_tempty = smem_u32(&bars[2 * kStages + 2]); // used in the leader CTA only
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const bool leader = rank == 0;
+    if (threadIdx.x == 0) {
+        s_abort = 0;
+        for (int i = 0; i < kStages; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(bar_tfull + 8 * i, 1); mbar_init(bar_tempty + 8 * i, 8); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc_pair(smem_u32(&s_tmem_base), 512);
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem_base = s_tmem_base;
+    volatile int *abort_flag = &s_abort;
+    pdl_wait();
+    const int n_live = __ldcg(a.meta_live);
+    const int n_rb = (n_live + kTile - 1) / kTile;
+    const int n_blocks = block_count<MODE>(a, n_rb);
+    const int cluster = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
+    const uint32_t full0 = mapa(bar_full, 0), tempty0 = mapa(bar_tempty, 0);
+    bool ok = true;
+    int code = 0;
+
+    if (warp == 0 || warp == 2) {
+        // ------------------------------------------------------------------ TMA producers
+        const bool is_a = warp == 0;
+        asm volatile("fence.proxy.async;" ::: "memory");  // what the kernels in front wrote is read through the async proxy
+        uint32_t s = 0, ph = 0;
+        for (int i = cluster; i < n_blocks && ok; i += n_clusters) {
+            const Block b = block_at<MODE>(a, i, n_live, n_rb);
+            for (int k = b.k0; k < b.k0 + b.ks; ++k) {
+                ok = __all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * s, ph ^ 1u, abort_flag));
+                if (!ok) break;
+                const uint32_t dst = ring + s * kStageBytes + (is_a ? 0 : kOperandBytes);
+                const uint32_t full = full0 + 8 * s;
+                if (elect_one()) {
+                    if (is_a) {
+                        if (leader) mbar_expect_tx(bar_full + 8 * s, 2 * kStageBytes);  // both operands, both CTAs
+                        if (MODE != kModeGrads) tma_load_2d_pair(dst, &maps.x_k, k * kBlockK, b.m * kTile + 128 * (int)rank, full);
+                        else if (b.slice >= 0) tma_load_2d_pair(dst, &maps.g_k, k * kBlockK, b.m * kTile + 128 * (int)rank, full);
+                        else tma_load_3d_pair(dst, &maps.g_mn, 0, k * kBlockK, 4 * b.m + 2 * (int)rank, full);
+                    } else {
+                        if (MODE != kModeGrads) tma_load_2d_pair(dst, &maps.w_k, k * kBlockK, a.v0 + b.n * kTile + 128 * (int)rank, full);
+                        else if (b.slice >= 0) tma_load_3d_pair(dst, &maps.w_mn, 0, a.v0 + k * kBlockK, 4 * b.n + 2 * (int)rank, full);
+                        else tma_load_3d_pair(dst, &maps.x_mn, 0, k * kBlockK, 4 * b.n + 2 * (int)rank, full);
+                    }
+                }
+                __syncwarp();
+                if (++s == kStages) { s = 0; ph ^= 1u; }
+            }
+        }
+        code = 31;
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer (leader CTA)
+        if (leader) {
+            uint32_t s = 0, ph = 0, count = 0;
+            for (int i = cluster; i < n_blocks && ok; i += n_clusters) {
+                const Block b = block_at<MODE>(a, i, n_live, n_rb);
+                if (MODE == kModeGrads && b.slice >= 0 && b.ks == 0) continue;  // an empty slice of a short piece adds nothing
+                const bool a_mn = MODE == kModeGrads && b.slice < 0, b_mn = MODE == kModeGrads;
+                const uint32_t idesc = instr_desc_pair(kTile) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
+                const uint64_t a0 = a_mn ? smem_desc_sw128_mn(ring) : smem_desc_sw128(ring);
+                const uint64_t b0 = b_mn ? smem_desc_sw128_mn(ring + kOperandBytes) : smem_desc_sw128(ring + kOperandBytes);
+                // a 16-element slice of the reduction axis: 32 bytes further in the swizzle row, or two 8-step groups
+                const uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
+                const uint32_t buf = count & 1u, tph = (count >> 1) & 1u;
+                ++count;
+                ok = __all_sync(0xffffffffu, mbar_wait(bar_tempty + 8 * buf, tph ^ 1u, abort_flag));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t dcol = tmem_base + buf * kTile;
+                for (int k = 0; k < b.ks; ++k) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * s, ph, abort_flag));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t da = a0 + (uint64_t)(s * (kStageBytes >> 4)), db = b0 + (uint64_t)(s * (kStageBytes >> 4));
+                    if (elect_one()) {
+#pragma unroll
+                        for (int j = 0; j < kBlockK / 16; ++j)
+                            umma_bf16_pair(dcol, da + j * a_step, db + j * b_step, idesc, (k | j) ? 1u : 0u);
+                        umma_commit_pair(bar_empty + 8 * s);
+                    }
+                    __syncwarp();
+                    if (++s == kStages) { s = 0; ph ^= 1u; }
+                }
+                if (!ok) break;
+                if (elect_one()) umma_commit_pair(bar_tfull + 8 * buf);
+                __syncwarp();
+            }
+            code = 32;
+        }
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------------ epilogue
+        const int q = warp & 3;
+        PatchWriter out = {patches + (uint32_t)q * 2 * kStoreBytes, lane, 0};
+        uint32_t count = 0;
+        for (int i = cluster; i < n_blocks && ok; i += n_clusters) {
+            const Block b = block_at<MODE>(a, i, n_live, n_rb);
+            if (MODE == kModeGrads && b.slice >= 0 && b.ks == 0) continue;
+            const uint32_t buf = count & 1u, tph = (count >> 1) & 1u;
+            ++count;
+            const int row = b.m * kTile + 128 * (int)rank + 32 * q + lane;  // of the block's rows, this thread's
+            const int v_first = a.v0 + b.n * kTile;                         // logits: vocabulary row of column 0
+            int label = -1;
+            float lse2 = 0.f, g = 0.f, gl = 0.f;
+            if (MODE != kModeGrads && row < n_live) {
+                label = __ldcg(a.row_target + row) - v_first;  // column of the target, if it is one of the block's
+                if (MODE == kModeDl) {
+                    lse2 = __ldcg(a.row_lse2 + row);
+                    g = __ldcg(a.row_g + row);
+                    gl = __ldcg(a.row_gl + row);
+                }
+            }
+            ok = __all_sync(0xffffffffu, mbar_wait(bar_tfull + 8 * buf, tph, abort_flag));
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t t0 = tmem_base + ((uint32_t)(32 * q) << 16) + buf * kTile;
+            auto release = [&]() {  // behind the last read of this accumulator
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * buf);
+            };
+            if (MODE == kModeNll) {
+                float m2 = -INFINITY, sum = 0.f;  // of the logits in units of ln 2, without the target's
+                for (int c0 = 0; c0 < kTile; c0 += 32) {
+                    float v[32];
+                    tmem_ld32(t0 + c0, v);
+                    if (c0 + 32 == kTile) release();
+                    const unsigned hit = (unsigned)(label - c0);
+                    if (__any_sync(0xffffffffu, hit < 32u)) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (hit == (unsigned)j) {
+                                a.row_label[row] = v[j];
+                                v[j] = -INFINITY;
+                            }
+                    }
+                    if (v_first + c0 + 32 > a.V) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (v_first + c0 + j >= a.V) v[j] = -INFINITY;
+                    }
+                    float top = v[0];
+#pragma unroll
+                    for (int j = 1; j < 32; ++j) top = fmaxf(top, v[j]);
+                    const float m_new = fmaxf(m2, top * kLog2e);
+                    const float ref = m_new == -INFINITY ? 0.f : m_new;
+                    float s4[4] = {sum * exp2_fast(m2 - ref), 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) s4[j & 3] += exp2_fast(fmaf(v[j], kLog2e, -ref));
+                    sum = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                    m2 = m_new;
+                }
+                if (row < n_live) a.part[(size_t)b.n * a.part_ld + row] = make_float2(m2, sum);
+            } else if (MODE == kModeDl) {
+                const bool live = row < n_live;
+                for (int c0 = 0; c0 < kTile; c0 += 64) {
+                    const uint32_t patch = out.begin();
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        float v[32];
+                        tmem_ld32(t0 + c0 + 32 * half, v);
+                        if (c0 + 64 == kTile && half == 1) release();
+                        const int c = c0 + 32 * half;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = live ? g * exp2_fast(fmaf(v[j], kLog2e, -lse2)) : 0.f;
+                        const unsigned hit = (unsigned)(label - c);
+                        if (__any_sync(0xffffffffu, hit < 32u)) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (hit == (unsigned)j) v[j] = gl;
+                        }
+                        if (v_first + c + 32 > a.V) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (v_first + c + j >= a.V) v[j] = 0.f;
+                        }
+#pragma unroll
+                        for (int p = 0; p < 4; ++p)
+                            out.put(patch, 4 * half + p, make_uint4(pack_bf16(v[8 * p], v[8 * p + 1]), pack_bf16(v[8 * p + 2], v[8 * p + 3]),
+                                                                    pack_bf16(v[8 * p + 4], v[8 * p + 5]), pack_bf16(v[8 * p + 6], v[8 * p + 7])));
+                    }
+                    out.end([&]() { tma_store_2d(&maps.g_store, b.n * kTile + c0, b.m * kTile + 128 * (int)rank + 32 * q, patch); });
+                }
+            } else if (b.slice >= 0) {
+                const int row0 = b.slice * a.dx_pitch + b.m * kTile + 128 * (int)rank + 32 * q;
+                for (int c0 = 0; c0 < kTile; c0 += 32) {
+                    if (b.n * kTile + c0 >= a.d) break;
+                    const uint32_t patch = out.begin();
+                    float v[32];
+                    tmem_ld32(t0 + c0, v);
+#pragma unroll
+                    for (int p = 0; p < 8; ++p)
+                        out.put(patch, p, make_uint4(__float_as_uint(v[4 * p]), __float_as_uint(v[4 * p + 1]), __float_as_uint(v[4 * p + 2]),
+                                                     __float_as_uint(v[4 * p + 3])));
+                    out.end([&]() {
+                        if (a.first) tma_store_2d(&maps.dx_store, b.n * kTile + c0, row0, patch);
+                        else tma_add_2d(&maps.dx_store, b.n * kTile + c0, row0, patch);
+                    });
+                }
+                release();
+            } else {
+                const int v_row0 = a.v0 + b.m * kTile + 128 * (int)rank + 32 * q;
+                for (int c0 = 0; c0 < kTile; c0 += 64) {
+                    if (b.n * kTile + c0 >= a.d || v_row0 >= a.V) break;
+                    const uint32_t patch = out.begin();
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        float v[32];
+                        tmem_ld32(t0 + c0 + 32 * half, v);
+                        if (b.ks == 0) {  // no token carries loss: nothing was accumulated
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[j] = 0.f;
+                        }
+#pragma unroll
+                        for (int p = 0; p < 4; ++p)
+                            out.put(patch, 4 * half + p, make_uint4(pack_bf16(v[8 * p], v[8 * p + 1]), pack_bf16(v[8 * p + 2], v[8 * p + 3]),
+                                                                    pack_bf16(v[8 * p + 4], v[8 * p + 5]), pack_bf16(v[8 * p + 6], v[8 * p + 7])));
+                    }
+                    out.end([&]() { tma_store_2d(&map_gw, b.n * kTile + c0, v_row0, patch); });
+                }
+                release();
+            }
+        }
+        if (lane == 0) bulk_wait_all();
+        code = 33;
+    }
+    if (!ok && lane == 0) {
+        if (!*abort_flag) atomicExch(&a.meta[kVocabError], code);
+        s_abort = 1;
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc_pair(tmem_base, 512);
+    }
+}
+
+struct RowArgs {
+    const __nv_bfloat16 *x;
+    const int32_t *target;
+    int T, V, d;
+    __nv_bfloat16 *xc;
+    int32_t *meta_live, *row_token, *row_target;
+    float *nll, *lse;                              // forward: zeros for tokens without a target
+    const float *nll_in, *lse_in, *grad_in;        // backward
+    float *row_lse2, *row_g, *row_gl;
+    __nv_bfloat16 *grad_x;                         // backward: zeros for tokens without a target
+};
+
+// Rows that carry loss to the front, in their order: each CTA counts the targets in front of its share of the tokens (all
+// of them once, from L2) and copies its rows.  For the gradients the last row block is filled up with zeros: its rows are
+// reduction steps of grad_w.
+template <bool BACKWARD>
+__global__ void __launch_bounds__(kRowThreads)
+vocab_rows_kernel(const RowArgs a, int token_ctas) {
+    pdl_launch_dependents();
+    __shared__ int s_sum[2][kRowThreads / 32];
+    __shared__ int s_row[kRowThreads];
+    pdl_wait();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int share = (a.T + token_ctas - 1) / token_ctas;
+    const int t0 = min(blockIdx.x * share, a.T), t1 = min(t0 + share, a.T);
+    auto live_at = [&](int t) { return (unsigned)__ldcg(a.target + t) < (unsigned)a.V; };
+    int before = 0, total = 0;
+#pragma unroll 8
+    for (int t = tid; t < a.T; t += kRowThreads) {
+        const int l = live_at(t) ? 1 : 0;
+        total += l;
+        before += t < t0 ? l : 0;
+    }
+    before = __reduce_add_sync(0xffffffffu, before);
+    total = __reduce_add_sync(0xffffffffu, total);
+    if (lane == 0) { s_sum[0][warp] = before; s_sum[1][warp] = total; }
+    __syncthreads();
+    before = total = 0;
+    for (int w = 0; w < kRowThreads / 32; ++w) { before += s_sum[0][w]; total += s_sum[1][w]; }
+    if (blockIdx.x == 0 && tid == 0) *a.meta_live = total;
+    const int chunks = a.d / 8;
+    for (int sub = t0; sub < t1; sub += kRowThreads) {
+        __syncthreads();
+        const int t = sub + tid;
+        const bool live = t < t1 && live_at(t);
+        const unsigned vote = __ballot_sync(0xffffffffu, live);
+        if (lane == 0) s_sum[0][warp] = __popc(vote);
+        __syncthreads();
+        int row = before + __popc(vote & ((1u << lane) - 1u));
+        for (int w = 0; w < kRowThreads / 32; ++w) {
+            if (w < warp) row += s_sum[0][w];
+            before += s_sum[0][w];
+        }
+        if (t < t1) {
+            if (live) {
+                a.row_token[row] = t;
+                a.row_target[row] = __ldcg(a.target + t);
+                if (BACKWARD) {
+                    const float g = __ldcg(a.grad_in + t);
+                    a.row_lse2[row] = __ldcg(a.lse_in + t) * kLog2e;
+                    a.row_g[row] = g;
+                    a.row_gl[row] = g * expm1f(-__ldcg(a.nll_in + t));
+                }
+            } else if (!BACKWARD) {
+                a.nll[t] = 0.f;
+                a.lse[t] = 0.f;
+            }
+        }
+        s_row[tid] = live ? row : -1;
+        __syncthreads();
+        for (int i = warp; i < min(kRowThreads, t1 - sub); i += kRowThreads / 32) {
+            const int r = s_row[i];
+            if (r >= 0) {
+                const uint4 *src = reinterpret_cast<const uint4 *>(a.x + (size_t)(sub + i) * a.d);
+                uint4 *dst = reinterpret_cast<uint4 *>(a.xc + (size_t)r * a.d);
+#pragma unroll 4
+                for (int c = lane; c < chunks; c += 32) dst[c] = __ldcg(src + c);
+            } else if (BACKWARD) {
+                uint4 *dst = reinterpret_cast<uint4 *>(a.grad_x + (size_t)(sub + i) * a.d);
+                for (int c = lane; c < chunks; c += 32) dst[c] = make_uint4(0, 0, 0, 0);
+            }
+        }
+    }
+    if (BACKWARD) {
+        const int end = (total + kTile - 1) / kTile * kTile;
+        for (int r = total + blockIdx.x * (kRowThreads / 32) + warp; r < end; r += gridDim.x * (kRowThreads / 32)) {
+            uint4 *dst = reinterpret_cast<uint4 *>(a.xc + (size_t)r * a.d);
+            for (int c = lane; c < chunks; c += 32) dst[c] = make_uint4(0, 0, 0, 0);
+        }
+    }
+}
+
+// The partial maxima and sums of a token's logits, and its likelihood.  A warp takes every sixteenth block of 256 logits
+// of 32 rows (a lane each).  The target's logit was kept apart: nll = log(1 + sum of the others' exp(l - l_target)) keeps
+// its digits where the target is nearly certain.
+constexpr int kNllWarps = 16;
+__global__ void __launch_bounds__(32 * kNllWarps)
+vocab_nll_kernel(const int32_t *__restrict__ meta_live, const float2 *__restrict__ part, int part_ld, int n_vt,
+                 const int32_t *__restrict__ row_token, const float *__restrict__ row_label, float *__restrict__ nll,
+                 float *__restrict__ lse) {
+    pdl_launch_dependents();
+    __shared__ float2 sh[kNllWarps][32];
+    pdl_wait();
+    const int n_live = __ldcg(meta_live);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int row = blockIdx.x * 32 + lane;
+    auto join = [](float2 &acc, float2 p) {
+        const float m = fmaxf(acc.x, p.x), ref = m == -INFINITY ? 0.f : m;
+        acc = make_float2(m, acc.y * exp2_fast(acc.x - ref) + p.y * exp2_fast(p.x - ref));
+    };
+    float2 acc = make_float2(-INFINITY, 0.f);
+    if (row < n_live) {
+#pragma unroll 8
+        for (int b = warp; b < n_vt; b += kNllWarps) join(acc, __ldcg(part + (size_t)b * part_ld + row));
+    }
+    sh[warp][lane] = acc;
+    __syncthreads();
+    if (warp != 0 || row >= n_live) return;
+    for (int w = 1; w < kNllWarps; ++w) join(acc, sh[w][lane]);
+    const float at = __ldcg(row_label + row);
+    const float ahead = fmaf(at, -kLog2e, acc.x);  // of the others' largest logit, in units of ln 2
+    const float loss = ahead > 0.f ? (ahead + log2f(acc.y + exp2f(-ahead))) * kLn2 : log1pf(acc.y * exp2f(ahead));
+    const int t = __ldcg(row_token + row);
+    nll[t] = loss;
+    lse[t] = at + loss;
+}
+
+// grad_x: the slices' sums of a row, rounded, to its token
+__global__ void __launch_bounds__(kRowThreads)
+vocab_grad_x_kernel(const int32_t *__restrict__ meta_live, const float *__restrict__ dx, int splits, size_t slice_stride, int d,
+                    const int32_t *__restrict__ row_token, __nv_bfloat16 *__restrict__ grad_x) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int n_live = __ldcg(meta_live);
+    const int lane = threadIdx.x & 31;
+    for (int r = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5); r < n_live; r += gridDim.x * (kRowThreads / 32)) {
+        const int t = __ldcg(row_token + r);
+        const float *src = dx + (size_t)r * d;
+        for (int c = lane; c < d / 8; c += 32) {
+            float4 lo = __ldcg(reinterpret_cast<const float4 *>(src) + 2 * c), hi = __ldcg(reinterpret_cast<const float4 *>(src) + 2 * c + 1);
+            for (int s = 1; s < splits; ++s) {
+                const float4 *p = reinterpret_cast<const float4 *>(src + s * slice_stride) + 2 * c;
+                const float4 l = __ldcg(p), h = __ldcg(p + 1);
+                lo.x += l.x; lo.y += l.y; lo.z += l.z; lo.w += l.w;
+                hi.x += h.x; hi.y += h.y; hi.z += h.z; hi.w += h.w;
+            }
+            *(reinterpret_cast<uint4 *>(grad_x + (size_t)t * d) + c) =
+                make_uint4(pack_bf16(lo.x, lo.y), pack_bf16(lo.z, lo.w), pack_bf16(hi.x, hi.y), pack_bf16(hi.z, hi.w));
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------- host
+inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+inline int tiles(int n) { return (n + kTile - 1) / kTile; }
+
+bool vocab_config_ok(const zeda_vocab_config_t *c, bool *shape) {
+    const char *w = nullptr;
+    *shape = false;
+    if (!c) w = "config is NULL";
+    else if (c->d_model < 64 || c->d_model % 64 || c->d_model > 8192) { w = "d_model must be a multiple of 64 in [64, 8192]"; *shape = true; }
+    else if (c->n_vocab < 1 || c->n_vocab > (1 << 24)) { w = "n_vocab must be in [1, 2^24]"; *shape = true; }
+    else if (c->max_tokens < 1 || c->max_tokens > (1 << 20)) w = "max_tokens must be in [1, 2^20]";
+    else if (c->backward != 0 && c->backward != 1) w = "backward must be 0 or 1";
+    else if (c->flags & ~ZEDA_FLAG_NO_DEPENDENT_LAUNCH) w = "unknown flag";
+    if (w) set_error("%s", w);
+    return w == nullptr;
+}
+
+// Slices of the vocabulary axis in which grad_x is summed, so that few row blocks still cover the SMs.
+int grad_x_splits(int T, int d, int kp) {
+    const int blocks = tiles(T) * tiles(d);
+    int s = 148 / blocks;
+    if (s > kMaxSplits) s = kMaxSplits;
+    const int steps = (kp + kBlockK - 1) / kBlockK;
+    if (s > steps) s = steps;
+    return s < 1 ? 1 : s;
+}
+
+size_t vocab_carve(const zeda_vocab_config_t &c, unsigned char *base, zeda_vocab *h) {
+    size_t off = 0;
+    auto take = [&](size_t bytes) -> void * {
+        void *p = base ? base + off : nullptr;
+        off = up256(off + bytes);
+        return p;
+    };
+    zeda_vocab v = {};
+    v.rows = tiles(c.max_tokens) * kTile;
+    // pieces of equal size, as few as keep dl within its bound
+    size_t cols = kPieceBytes / ((size_t)v.rows * 2) / kTile * kTile;
+    if (cols < kTile) cols = kTile;
+    const int all = tiles(c.n_vocab) * kTile;
+    const int pieces = (int)((all + cols - 1) / cols);
+    v.piece = tiles((all + pieces - 1) / pieces) * kTile;
+    const int few = 148 / tiles(c.d_model) + 1;
+    v.dx_rows = kTile * (tiles(c.max_tokens) > few ? tiles(c.max_tokens) : few);
+    v.meta = (int32_t *)take(kVocabMetaCount * 4);
+    v.row_token = (int32_t *)take((size_t)v.rows * 4);
+    v.row_target = (int32_t *)take((size_t)v.rows * 4);
+    v.row_label = (float *)take((size_t)v.rows * 4);
+    v.part = (float2 *)take((size_t)tiles(c.n_vocab) * v.rows * 8);
+    v.xc = (__nv_bfloat16 *)take((size_t)v.rows * c.d_model * 2);
+    if (c.backward) {
+        v.row_lse2 = (float *)take((size_t)v.rows * 4);
+        v.row_g = (float *)take((size_t)v.rows * 4);
+        v.row_gl = (float *)take((size_t)v.rows * 4);
+        v.g = (__nv_bfloat16 *)take((size_t)v.rows * v.piece * 2);
+        v.dx = (float *)take((size_t)v.dx_rows * c.d_model * 4);
+    }
+    if (h) {
+        v.cfg = h->cfg;
+        v.pdl = h->pdl;
+        v.sm_count = h->sm_count;
+        v.w = h->w;
+        v.maps = h->maps;
+        *h = v;
+    }
+    return off;
+}
+
+bool map_2d(CUtensorMap *m, const void *base, size_t rows, size_t cols, int box_cols, int box_rows) {
+    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {cols * 2};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
+    return encode_bf16_map(m, base, 2, dims, strides, box);
+}
+
+// [steps][cols] with the columns in blocks of 64: one box holds 64 steps of two blocks, block after block
+bool map_mn(CUtensorMap *m, const void *base, size_t steps, size_t cols) {
+    const cuuint64_t dims[3] = {64, steps, cols / 64}, strides[2] = {cols * 2, 128};
+    const cuuint32_t box[3] = {64, kBlockK, 2};
+    return encode_bf16_map(m, base, 3, dims, strides, box);
+}
+
+bool build_maps(zeda_vocab *h, VocabMaps *m) {
+    const size_t d = h->cfg.d_model, V = h->cfg.n_vocab;
+    bool ok = map_2d(&m->x_k, h->xc, h->rows, d, kBlockK, 128) && map_2d(&m->w_k, h->w, V, d, kBlockK, 128);
+    if (ok && h->cfg.backward) {
+        ok = map_2d(&m->g_k, h->g, h->rows, h->piece, kBlockK, 128) && map_mn(&m->x_mn, h->xc, h->rows, d) && map_mn(&m->w_mn, h->w, V, d) &&
+             map_mn(&m->g_mn, h->g, h->rows, h->piece) && map_2d(&m->g_store, h->g, h->rows, h->piece, 64, 32);
+        const cuuint64_t dims[2] = {d, (cuuint64_t)h->dx_rows}, strides[1] = {d * 4};
+        const cuuint32_t box[2] = {32, 32};
+        ok = ok && encode_f32_map(&m->dx_store, h->dx, 2, dims, strides, box);
+    }
+    return ok;
+}
+
+template <int MODE>
+cudaError_t launch_gemm(const zeda_vocab *h, const CUtensorMap &map_gw, const GemmArgs &a, cudaStream_t s) {
+    return launch_kernel(h->pdl, vocab_gemm_kernel<MODE>, dim3(h->sm_count / 2 * 2), dim3(kGemmThreads), (size_t)kGemmSmem, s,
+                         *static_cast<const VocabMaps *>(h->maps), map_gw, a);
+}
+
+template <bool BACKWARD>
+cudaError_t launch_rows(const zeda_vocab *h, RowArgs &a, cudaStream_t s) {
+    int token_ctas = (a.T + 15) / 16;
+    if (token_ctas > 2 * h->sm_count) token_ctas = 2 * h->sm_count;
+    const int ctas = BACKWARD && token_ctas < 32 ? 32 : token_ctas;  // the others help with the zeros behind the last row
+    a.V = h->cfg.n_vocab;
+    a.d = h->cfg.d_model;
+    a.xc = h->xc;
+    a.meta_live = h->meta + kLive;
+    a.row_token = h->row_token;
+    a.row_target = h->row_target;
+    a.row_lse2 = h->row_lse2;
+    a.row_g = h->row_g;
+    a.row_gl = h->row_gl;
+    return launch_kernel(h->pdl, vocab_rows_kernel<BACKWARD>, dim3(ctas), dim3(kRowThreads), 0, s, a, token_ctas);
+}
+
+GemmArgs gemm_args(const zeda_vocab *h) {
+    GemmArgs a = {};
+    a.d = h->cfg.d_model;
+    a.V = h->cfg.n_vocab;
+    a.kp = h->cfg.n_vocab;
+    a.meta_live = h->meta + kLive;
+    a.meta = h->meta;
+    a.row_target = h->row_target;
+    a.row_label = h->row_label;
+    a.row_lse2 = h->row_lse2;
+    a.row_g = h->row_g;
+    a.row_gl = h->row_gl;
+    a.part = h->part;
+    a.part_ld = h->rows;
+    return a;
+}
+
+zeda_status_t vocab_fail(const char *what, cudaError_t e) {
+    set_error("%s: %s", what, cudaGetErrorString(e));
+    return ZEDA_ERR_CUDA;
+}
+
+bool unaligned(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
+
+zeda_status_t vocab_call_ok(const zeda_vocab *h, int T) {
+    if (!h) { set_error("handle is NULL"); return ZEDA_ERR_INVALID_ARG; }
+    if (T < 0 || T > h->cfg.max_tokens) { set_error("T=%d outside [0, max_tokens=%d]", T, h->cfg.max_tokens); return ZEDA_ERR_INVALID_ARG; }
+    return ZEDA_OK;
+}
+
+const char kVocabFailure[] = "a bounded device wait expired (code %d)";
+
+}  // namespace
+
+}  // namespace zeda
+
+using namespace zeda;
+
+extern "C" {
+
+size_t zeda_vocab_workspace_bytes(const zeda_vocab_config_t *cfg) {
+    bool shape;
+    return vocab_config_ok(cfg, &shape) ? vocab_carve(*cfg, nullptr, nullptr) : 0;
+}
+
+zeda_status_t zeda_vocab_create(const zeda_vocab_config_t *cfg, const void *w, void *workspace, size_t workspace_bytes,
+                                zeda_vocab_t **out) {
+    if (out) *out = nullptr;
+    bool shape;
+    if (!vocab_config_ok(cfg, &shape)) return shape ? ZEDA_ERR_UNSUPPORTED : ZEDA_ERR_INVALID_ARG;
+    if (!out) { set_error("out is NULL"); return ZEDA_ERR_INVALID_ARG; }
+    if (!w || !workspace) { set_error("a required pointer is NULL"); return ZEDA_ERR_INVALID_ARG; }
+    if (unaligned(w, 16)) { set_error("w must be 16-byte aligned"); return ZEDA_ERR_INVALID_ARG; }
+    if (unaligned(workspace, 256)) { set_error("workspace must be 256-byte aligned"); return ZEDA_ERR_INVALID_ARG; }
+    const size_t need = vocab_carve(*cfg, nullptr, nullptr);
+    if (workspace_bytes < need) { set_error("workspace has %zu bytes, %zu needed", workspace_bytes, need); return ZEDA_ERR_WORKSPACE; }
+    int ndev = 0;
+    cudaError_t e = cudaGetDeviceCount(&ndev);
+    if (e != cudaSuccess) return vocab_fail("cudaGetDeviceCount", e);
+    if (cfg->device < 0 || cfg->device >= ndev) { set_error("device %d not present (%d devices)", cfg->device, ndev); return ZEDA_ERR_INVALID_ARG; }
+    if ((e = cudaSetDevice(cfg->device)) != cudaSuccess) return vocab_fail("cudaSetDevice", e);
+    cudaDeviceProp prop;
+    if ((e = cudaGetDeviceProperties(&prop, cfg->device)) != cudaSuccess) return vocab_fail("cudaGetDeviceProperties", e);
+    if (prop.major != 10) { set_error("this library is built for sm_100a only; device is sm_%d%d", prop.major, prop.minor); return ZEDA_ERR_UNSUPPORTED; }
+    zeda_vocab *h = new (std::nothrow) zeda_vocab();
+    VocabMaps *maps = static_cast<VocabMaps *>(aligned_alloc(64, sizeof(VocabMaps)));
+    if (!h || !maps) {
+        delete h;
+        free(maps);
+        set_error("out of host memory");
+        return ZEDA_ERR_INVALID_ARG;
+    }
+    memset(maps, 0, sizeof *maps);
+    h->cfg = *cfg;
+    h->pdl = !(cfg->flags & ZEDA_FLAG_NO_DEPENDENT_LAUNCH);
+    h->sm_count = prop.multiProcessorCount;
+    h->w = static_cast<const __nv_bfloat16 *>(w);
+    h->maps = maps;
+    vocab_carve(*cfg, static_cast<unsigned char *>(workspace), h);
+    zeda_status_t st = ZEDA_OK;
+    if (!build_maps(h, maps)) st = ZEDA_ERR_CUDA;
+    const void *kernels[3] = {(const void *)vocab_gemm_kernel<kModeNll>, (const void *)vocab_gemm_kernel<kModeDl>,
+                              (const void *)vocab_gemm_kernel<kModeGrads>};
+    for (const void *k : kernels)
+        if (st == ZEDA_OK && (e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem)) != cudaSuccess)
+            st = vocab_fail("kernel set-up", e);
+    if (st == ZEDA_OK && (e = cudaMemset(h->meta, 0, kVocabMetaCount * 4)) != cudaSuccess) st = vocab_fail("cudaMemset(meta)", e);
+    if (st == ZEDA_OK && (e = cudaDeviceSynchronize()) != cudaSuccess) st = vocab_fail("cudaDeviceSynchronize", e);
+    if (st != ZEDA_OK) {
+        free(maps);
+        delete h;
+        return st;
+    }
+    *out = h;
+    return ZEDA_OK;
+}
+
+zeda_status_t zeda_vocab_nll(zeda_vocab_t *h, const void *x, const int32_t *target, int32_t T, float *nll, float *lse, void *stream) {
+    zeda_status_t st = vocab_call_ok(h, T);
+    if (st != ZEDA_OK || T == 0) return st;
+    if (!x || !target || !nll || !lse) { set_error("x, target, nll and lse are required"); return ZEDA_ERR_INVALID_ARG; }
+    if (unaligned(x, 16) || unaligned(target, 4) || unaligned(nll, 4) || unaligned(lse, 4)) {
+        set_error("x must be 16-byte aligned, the other arrays 4-byte");
+        return ZEDA_ERR_INVALID_ARG;
+    }
+    cudaError_t e = cudaSetDevice(h->cfg.device);
+    if (e != cudaSuccess) return vocab_fail("cudaSetDevice", e);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    RowArgs r = {};
+    r.x = static_cast<const __nv_bfloat16 *>(x);
+    r.target = target;
+    r.T = T;
+    r.nll = nll;
+    r.lse = lse;
+    if ((e = launch_rows<false>(h, r, s)) != cudaSuccess) return vocab_fail("row gather launch", e);
+    const GemmArgs a = gemm_args(h);
+    const VocabMaps *maps = static_cast<const VocabMaps *>(h->maps);
+    if ((e = launch_gemm<kModeNll>(h, maps->x_k, a, s)) != cudaSuccess) return vocab_fail("logits launch", e);
+    e = launch_kernel(h->pdl, vocab_nll_kernel, dim3((T + 31) / 32), dim3(32 * kNllWarps), 0, s, (const int32_t *)(h->meta + kLive),
+                      (const float2 *)h->part, h->rows, tiles(h->cfg.n_vocab), (const int32_t *)h->row_token, (const float *)h->row_label, nll, lse);
+    if (e != cudaSuccess) return vocab_fail("likelihood launch", e);
+    return ZEDA_OK;
+}
+
+zeda_status_t zeda_vocab_nll_backward(zeda_vocab_t *h, const void *x, const int32_t *target, int32_t T, const float *nll, const float *lse,
+                                      const float *grad_nll, void *grad_x, void *grad_w, void *stream) {
+    zeda_status_t st = vocab_call_ok(h, T);
+    if (st != ZEDA_OK) return st;
+    if (!h->cfg.backward) { set_error("the handle was not created for gradients (backward = 0)"); return ZEDA_ERR_INVALID_ARG; }
+    if (!grad_w || unaligned(grad_w, 16)) { set_error("grad_w is NULL or not 16-byte aligned"); return ZEDA_ERR_INVALID_ARG; }
+    const size_t w_bytes = (size_t)h->cfg.n_vocab * h->cfg.d_model * 2, x_bytes = (size_t)T * h->cfg.d_model * 2;
+    if (T > 0) {
+        if (!x || !target || !nll || !lse || !grad_nll || !grad_x) {
+            set_error("x, target, nll, lse, grad_nll and grad_x are required");
+            return ZEDA_ERR_INVALID_ARG;
+        }
+        if (unaligned(x, 16) || unaligned(grad_x, 16) || unaligned(target, 4) || unaligned(nll, 4) || unaligned(lse, 4) || unaligned(grad_nll, 4)) {
+            set_error("x and grad_x must be 16-byte aligned, the other arrays 4-byte");
+            return ZEDA_ERR_INVALID_ARG;
+        }
+    }
+    const char *reg[4] = {static_cast<const char *>(x), reinterpret_cast<const char *>(h->w), static_cast<const char *>(grad_x),
+                          static_cast<const char *>(grad_w)};
+    const size_t len[4] = {x_bytes, w_bytes, x_bytes, w_bytes};
+    for (int i = 0; i < 4; ++i)
+        for (int j = i < 2 ? 2 : i + 1; j < 4; ++j)
+            if (len[i] && len[j] && reg[i] < reg[j] + len[j] && reg[j] < reg[i] + len[i]) {
+                set_error("grad_x or grad_w overlaps another of x, w, grad_x, grad_w");
+                return ZEDA_ERR_INVALID_ARG;
+            }
+    cudaError_t e = cudaSetDevice(h->cfg.device);
+    if (e != cudaSuccess) return vocab_fail("cudaSetDevice", e);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (T == 0) {  // a sum over no tokens
+        e = cudaMemsetAsync(grad_w, 0, w_bytes, s);
+        return e == cudaSuccess ? ZEDA_OK : vocab_fail("cudaMemsetAsync", e);
+    }
+    CUtensorMap map_gw;
+    if (!map_2d(&map_gw, grad_w, h->cfg.n_vocab, h->cfg.d_model, 64, 32)) return ZEDA_ERR_CUDA;
+    RowArgs r = {};
+    r.x = static_cast<const __nv_bfloat16 *>(x);
+    r.target = target;
+    r.T = T;
+    r.nll_in = nll;
+    r.lse_in = lse;
+    r.grad_in = grad_nll;
+    r.grad_x = static_cast<__nv_bfloat16 *>(grad_x);
+    if ((e = launch_rows<true>(h, r, s)) != cudaSuccess) return vocab_fail("row gather launch", e);
+    GemmArgs a = gemm_args(h);
+    const int V = h->cfg.n_vocab;
+    a.splits = grad_x_splits(T, a.d, V < h->piece ? V : h->piece);
+    a.dx_pitch = tiles(T) * kTile;
+    for (int v0 = 0; v0 < V; v0 += h->piece) {
+        a.v0 = v0;
+        a.kp = V - v0 < h->piece ? V - v0 : h->piece;
+        a.first = v0 == 0;
+        if ((e = launch_gemm<kModeDl>(h, map_gw, a, s)) != cudaSuccess) return vocab_fail("logits' gradient launch", e);
+        if ((e = launch_gemm<kModeGrads>(h, map_gw, a, s)) != cudaSuccess) return vocab_fail("gradients launch", e);
+    }
+    int ctas = (T + kRowThreads / 32 - 1) / (kRowThreads / 32);
+    if (ctas > 8 * h->sm_count) ctas = 8 * h->sm_count;
+    e = launch_kernel(h->pdl, vocab_grad_x_kernel, dim3(ctas), dim3(kRowThreads), 0, s, (const int32_t *)(h->meta + kLive),
+                      (const float *)h->dx, a.splits, (size_t)a.dx_pitch * a.d, a.d, (const int32_t *)h->row_token,
+                      static_cast<__nv_bfloat16 *>(grad_x));
+    if (e != cudaSuccess) return vocab_fail("grad_x launch", e);
+    return ZEDA_OK;
+}
+
+zeda_status_t zeda_vocab_check(zeda_vocab_t *h, void *stream) {
+    if (!h) { set_error("handle is NULL"); return ZEDA_ERR_INVALID_ARG; }
+    cudaError_t e = cudaSetDevice(h->cfg.device);
+    if (e != cudaSuccess) return vocab_fail("cudaSetDevice", e);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    int32_t err = 0;
+    e = cudaMemcpyAsync(&err, h->meta + kVocabError, 4, cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (e != cudaSuccess) return vocab_fail("zeda_vocab_check", e);
+    if (err == 0) return ZEDA_OK;
+    e = cudaMemsetAsync(h->meta + kVocabError, 0, 4, s);
+    if (e != cudaSuccess) return vocab_fail("cudaMemsetAsync", e);
+    set_error(kVocabFailure, err);
+    return ZEDA_ERR_TIMEOUT;
+}
+
+zeda_status_t zeda_vocab_destroy(zeda_vocab_t *h) {
+    if (!h) return ZEDA_OK;
+    zeda_status_t st = ZEDA_OK;
+    if (cudaSetDevice(h->cfg.device) == cudaSuccess) {
+        int32_t err = 0;
+        cudaError_t e = cudaDeviceSynchronize();
+        if (e == cudaSuccess) e = cudaMemcpy(&err, h->meta + kVocabError, 4, cudaMemcpyDeviceToHost);
+        if (e != cudaSuccess) st = vocab_fail("zeda_vocab_destroy", e);
+        else if (err != 0) { set_error(kVocabFailure, err); st = ZEDA_ERR_TIMEOUT; }
+    }
+    free(h->maps);
+    delete h;
+    return st;
+}
+
+}  // extern "C"

@@ -28,7 +28,8 @@ EXPORTS = (
     "zeda_moe_balance_loss", "zeda_moe_router_backward", "zeda_moe_token_zero_share", "zeda_moe_last_counters", "zeda_moe_set_profiling", "zeda_moe_stage_ms", "zeda_residual_rmsnorm",
     "zeda_moe_selftest_wait", "zeda_moe_clear_error",
     "zeda_ep_dispatch", "zeda_ep_experts", "zeda_ep_combine",
-    "zeda_compact_static", "zeda_moe_destroy", "zeda_last_error", "zeda_version",
+    "zeda_vocab_workspace_bytes", "zeda_vocab_create", "zeda_vocab_nll", "zeda_vocab_nll_backward", "zeda_vocab_check",
+    "zeda_vocab_destroy", "zeda_compact_static", "zeda_moe_destroy", "zeda_last_error", "zeda_version",
 )
 
 
@@ -40,6 +41,10 @@ class Config(ctypes.Structure):
 
 class Balance(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int32), ("alpha", ctypes.c_float), ("group_w", ctypes.c_float)]
+
+
+class VocabConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("d_model", "n_vocab", "max_tokens", "backward", "device", "flags")]
 
 
 class ZedaError(RuntimeError):
@@ -97,6 +102,18 @@ def _load() -> ctypes.CDLL:
     lib.zeda_ep_experts.argtypes = [vp, vp, vp, i32, vp, vp]
     lib.zeda_ep_combine.restype = i32
     lib.zeda_ep_combine.argtypes = [vp, vp, vp, i32, vp, vp]
+    lib.zeda_vocab_workspace_bytes.restype = sz
+    lib.zeda_vocab_workspace_bytes.argtypes = [ctypes.POINTER(VocabConfig)]
+    lib.zeda_vocab_create.restype = i32
+    lib.zeda_vocab_create.argtypes = [ctypes.POINTER(VocabConfig), vp, vp, sz, ctypes.POINTER(vp)]
+    lib.zeda_vocab_nll.restype = i32
+    lib.zeda_vocab_nll.argtypes = [vp, vp, vp, i32, vp, vp, vp]
+    lib.zeda_vocab_nll_backward.restype = i32
+    lib.zeda_vocab_nll_backward.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.zeda_vocab_check.restype = i32
+    lib.zeda_vocab_check.argtypes = [vp, vp]
+    lib.zeda_vocab_destroy.restype = i32
+    lib.zeda_vocab_destroy.argtypes = [vp]
     lib.zeda_compact_static.restype = i32
     lib.zeda_compact_static.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp]
     lib.zeda_moe_destroy.restype = i32
@@ -406,6 +423,78 @@ class ZedaMoE:
     def _check_x(self, x: torch.Tensor) -> int:
         assert x.device == self.device and x.dtype == torch.bfloat16 and x.is_contiguous() and x.dim() == 2
         assert x.shape[1] == self.d
+        return x.shape[0]
+
+
+class VocabLoss:
+    """Token likelihoods under a vocabulary matrix w [n_vocab, d] bf16 (zeda_vocab_*).  Keeps references to w and the
+    workspace; the values of w may change between calls.  One stream at a time."""
+
+    def __init__(self, w: torch.Tensor, max_tokens: int, backward: bool = True, flags: int = FLAG_NONE,
+                 workspace: Optional[torch.Tensor] = None):
+        dev = w.device
+        assert dev.type == "cuda", "weights must live on a CUDA device"
+        assert w.dtype == torch.bfloat16 and w.dim() == 2 and w.is_contiguous()
+        self.cfg = VocabConfig(w.shape[1], w.shape[0], max_tokens, 1 if backward else 0,
+                               dev.index if dev.index is not None else torch.cuda.current_device(), flags)
+        need = int(lib.zeda_vocab_workspace_bytes(ctypes.byref(self.cfg)))
+        if need == 0:
+            raise ZedaError(ERR_INVALID_ARG, last_error())
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        self._keep = (w, workspace)
+        self.device, self.w = dev, w
+        self.V, self.d = w.shape
+        h = ctypes.c_void_p()
+        _check(lib.zeda_vocab_create(ctypes.byref(self.cfg), _ptr(w), _ptr(workspace), workspace.numel(), ctypes.byref(h)))
+        self._h = h
+
+    def nll(self, x: torch.Tensor, target: torch.Tensor):
+        """zeda_vocab_nll: (nll [T], lse [T]) fp32 of the targets [T] int32 (outside [0, n_vocab): no loss) given the
+        hidden states x [T, d] bf16; asynchronous on the current stream."""
+        T = self._check_inputs(x, target)
+        nll = torch.empty(T, dtype=torch.float32, device=self.device)
+        lse = torch.empty(T, dtype=torch.float32, device=self.device)
+        _check(lib.zeda_vocab_nll(self._h, _ptr(x), _ptr(target), T, _ptr(nll), _ptr(lse), _stream(self.device)))
+        return nll, lse
+
+    def backward(self, x: torch.Tensor, target: torch.Tensor, nll: torch.Tensor, lse: torch.Tensor, grad_nll: torch.Tensor,
+                 grad_x: Optional[torch.Tensor] = None, grad_w: Optional[torch.Tensor] = None):
+        """zeda_vocab_nll_backward: (grad_x [T, d], grad_w [n_vocab, d]) bf16 of sum_t grad_nll[t] nll[t], with nll and
+        lse as returned by ``nll`` for the same x, w and target; asynchronous on the current stream."""
+        T = self._check_inputs(x, target)
+        for t in (nll, lse, grad_nll):
+            assert t.device == self.device and t.dtype == torch.float32 and t.is_contiguous() and t.shape == (T,)
+        if grad_x is None:
+            grad_x = torch.empty_like(x)
+        if grad_w is None:
+            grad_w = torch.empty_like(self.w)
+        for g, like in ((grad_x, x), (grad_w, self.w)):
+            assert g.device == self.device and g.dtype == torch.bfloat16 and g.is_contiguous() and g.shape == like.shape
+        _check(lib.zeda_vocab_nll_backward(self._h, _ptr(x), _ptr(target), T, _ptr(nll), _ptr(lse), _ptr(grad_nll), _ptr(grad_x),
+                                           _ptr(grad_w), _stream(self.device)))
+        return grad_x, grad_w
+
+    def check(self):
+        """zeda_vocab_check: raises if a bounded device wait expired since the last check; synchronises."""
+        _check(lib.zeda_vocab_check(self._h, _stream(self.device)))
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            h, self._h = self._h, None
+            _check(lib.zeda_vocab_destroy(h))
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check_inputs(self, x, target) -> int:
+        assert x.device == self.device and x.dtype == torch.bfloat16 and x.is_contiguous() and x.dim() == 2
+        assert x.shape[1] == self.d
+        assert target.device == self.device and target.dtype == torch.int32 and target.is_contiguous()
+        assert target.shape == (x.shape[0],)
         return x.shape[0]
 
 

@@ -1,0 +1,290 @@
+"""Token likelihoods under a vocabulary matrix and their gradients, against a plain implementation in 64 bits.
+
+Tolerances.  A logit is an fp32 sum of d exact products, added up 16 at a time: off by at most (d / 16 + 4) 2^-23 of the sum
+of the products' magnitudes, call it e.  A likelihood differs by at most 2 e, plus roundings of numbers as large as the
+logits (8 of 2^-23 of the largest).  A logit's gradient is rounded to bf16 (2^-8 of it) behind an exponential that is off by
+2 e + 8e-6 relative; a gradient is the sum of such terms (fp32, 16 terms or more at a time) and rounded once more (2^-8).
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+HALF = 2.0 ** -8  # half a step of bf16, relative
+
+
+def make(T, d, V, seed, ignored=0.0, lean=0.6):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    w = (torch.randn(V, d, generator=g, device=DEV) * (0.9 / math.sqrt(d))).to(torch.bfloat16)
+    target = torch.randint(0, V, (T,), generator=g, device=DEV)
+    x = torch.randn(T, d, generator=g, device=DEV)
+    x += torch.rand(T, 1, generator=g, device=DEV) * lean * math.sqrt(d) * torch.nn.functional.normalize(w[target].float(), dim=1)
+    if ignored:
+        drop = torch.rand(T, generator=g, device=DEV) < ignored
+        target[drop] = -100
+    grad = (torch.rand(T, generator=g, device=DEV) - 0.3) / max(T, 1)
+    return x.to(torch.bfloat16), w, target.to(torch.int32), grad
+
+
+def reference(x, w, target, grad):
+    """(nll, lse, e, grad_x, grad_w, bounds of the gradients' errors), 64 bits; tokens without loss 0"""
+    V, d = w.shape
+    T = x.shape[0]
+    live = (target >= 0) & (target < V)
+    rows = torch.nonzero(live)[:, 0]
+    X, W = x[rows].double(), w.double()
+    l = X @ W.t()
+    lab = target[rows].long()
+    lse_r = torch.logsumexp(l, dim=1)
+    at = torch.arange(len(rows), device=DEV)
+    e = ((d / 16 + 4) * 2.0 ** -23 * (X.abs() @ W.abs().t()).amax(dim=1)) if len(rows) else l.new_zeros(0)
+    big = l.abs().amax(dim=1) if len(rows) else e
+    nll, lse, tol = (torch.zeros(T, dtype=torch.float64, device=DEV) for _ in range(3))
+    # log(1 + what the others add): lse - l would lose the likelihood of a nearly certain target to cancellation, in 64 bits too
+    others = l - l[at, lab][:, None]
+    others[at, lab] = -math.inf
+    nll_r = torch.logsumexp(torch.cat([others, torch.zeros_like(others[:, :1])], dim=1), dim=1)
+    sure = nll_r < 1
+    nll_r[sure] = torch.log1p(others[sure].exp().sum(dim=1))
+    nll[rows], lse[rows] = nll_r, lse_r
+    tol[rows] = 2 * e + 8 * 2.0 ** -23 * (big + 1)
+    p = torch.softmax(l, dim=1)
+    dl = p.clone()
+    dl[at, lab] = torch.expm1(-nll_r)
+    dl *= grad[rows].double()[:, None]
+    rel = HALF + 2 * e + 8e-6
+    # the target's own term: 1 - p, whose error is that of p
+    err_dl = dl.abs() * rel[:, None]
+    err_dl[at, lab] += grad[rows].double().abs() * p[at, lab] * (2 * e + 8e-6)
+    gx = torch.zeros((T, d), dtype=torch.float64, device=DEV)
+    ex = torch.zeros_like(gx)
+    gx[rows] = dl @ W
+    ex[rows] = (err_dl + dl.abs() * (V / 16 + 4) * 2.0 ** -23) @ W.abs() + HALF * 1.01 * gx[rows].abs()
+    gw = dl.t() @ X
+    ew = (err_dl + dl.abs() * (T / 16 + 4) * 2.0 ** -23).t() @ X.abs() + HALF * 1.01 * gw.abs()
+    return nll, lse, tol, gx, gw, ex, ew
+
+
+def check(zeda, m, x, w, target, grad, backward=True):
+    nll, lse = m.nll(x, target)
+    m.check()
+    r = reference(x, w, target, grad)
+    for got, want in ((nll, r[0]), (lse, r[1])):
+        bad = (got.double() - want).abs() > r[2]
+        assert not bad.any(), (got[bad], want[bad], r[2][bad])
+    if not backward:
+        return nll, lse
+    gx = torch.full_like(x, float("nan"))
+    gw = torch.full_like(w, float("nan"))
+    gx, gw = m.backward(x, target, nll, lse, grad, gx, gw)
+    m.check()
+    for got, want, tol in ((gx, r[3], r[5]), (gw, r[4], r[6])):
+        err = (got.double() - want).abs()
+        assert bool((err <= tol + 1e-36).all()), (float((err - tol).max()), int((err > tol).sum()))
+        # roundings are independent: two of at most 2^-8 / sqrt(3) rms each
+        if want.numel() > 4096 and bool(want.any()):
+            assert float(err.norm() / want.norm()) <= HALF
+    return nll, lse, gx, gw
+
+
+SIZES = [  # T, d, V, ignored
+    (1, 64, 1, 0.0), (1, 64, 2, 0.0), (3, 64, 31, 0.0), (2, 128, 256, 0.0), (64, 64, 257, 0.3), (65, 192, 1000, 0.0),
+    (255, 320, 511, 0.5), (256, 256, 512, 0.0), (257, 64, 4099, 0.1), (700, 1088, 2003, 0.4), (1, 2048, 20011, 0.0),
+    (33, 2048, 9000, 0.0), (1500, 512, 3001, 0.25), (300, 8192, 300, 0.0), (2049, 128, 700, 0.9),
+]
+
+
+@pytest.mark.parametrize("T,d,V,ignored", SIZES)
+def test_likelihood(T, d, V, ignored):
+    from paper_2605_18643_b200 import zeda
+    x, w, target, grad = make(T, d, V, seed=T + d + V, ignored=ignored)
+    m = zeda.VocabLoss(w, T, backward=False)
+    nll, lse = check(zeda, m, x, w, target, grad, backward=False)
+    again = m.nll(x, target)
+    assert torch.equal(nll, again[0]) and torch.equal(lse, again[1])
+    m.close()
+
+
+@pytest.mark.parametrize("T,d,V,ignored", SIZES)
+def test_gradients(T, d, V, ignored):
+    from paper_2605_18643_b200 import zeda
+    x, w, target, grad = make(T, d, V, seed=T + d + V + 1, ignored=ignored)
+    m = zeda.VocabLoss(w, T)
+    nll, lse, gx, gw = check(zeda, m, x, w, target, grad)
+    again = m.backward(x, target, nll, lse, grad)
+    assert torch.equal(gx, again[0]) and torch.equal(gw, again[1])
+    m.close()
+
+
+@pytest.mark.parametrize("T,V", [(300, 5000), (1, 4097), (513, 2049)])
+def test_gradients_over_several_pieces_of_the_vocabulary(T, V):
+    from paper_2605_18643_b200 import zeda
+    x, w, target, grad = make(T, 128, V, seed=T, ignored=0.2 if T > 1 else 0.0)
+    m = zeda.VocabLoss(w, 65536)   # a handle for many tokens keeps its pieces small: 2048 columns
+    check(zeda, m, x, w, target, grad)
+    m.close()
+
+
+def test_tokens_without_loss_are_left_out():
+    from paper_2605_18643_b200 import zeda
+    T, d, V = 400, 192, 777
+    x, w, target, grad = make(T, d, V, seed=11)
+    target[::4] = -100
+    target[1::8] = V            # beyond the vocabulary: no loss either
+    target[3::16] = -2 ** 31
+    target[5::16] = 2 ** 31 - 1
+    dead = (target < 0) | (target >= V)
+    m = zeda.VocabLoss(w, T)
+    a = check(zeda, m, x, w, target, grad)
+    x2, g2 = x.clone(), grad.clone()
+    x2[dead] = float("nan")
+    x2[torch.nonzero(dead)[::2, 0]] = float("inf")
+    g2[dead] = float("nan")
+    nll, lse = m.nll(x2, target)
+    gx, gw = m.backward(x2, target, nll, lse, g2)
+    assert all(torch.equal(p, q) for p, q in zip(a, (nll, lse, gx, gw)))
+    assert not nll[dead].any() and not lse[dead].any() and not gx[dead].any()
+    # a smaller call behind a larger one, and one where no token carries loss
+    check(zeda, m, x[:70].contiguous(), w, target[:70].contiguous(), grad[:70].contiguous())
+    none = torch.full((T,), -1, dtype=torch.int32, device=DEV)
+    nll, lse = m.nll(x2, none)
+    gx, gw = m.backward(x2, none, nll, lse, g2)
+    assert not nll.any() and not lse.any() and not gx.any() and not gw.any()
+    gw.fill_(float("nan"))
+    nll, lse = m.nll(x[:0], target[:0])
+    gx, gw = m.backward(x[:0], target[:0], nll, lse, grad[:0], grad_w=gw)
+    assert gx.shape == (0, d) and not gw.any()
+    m.check()
+    m.close()
+
+
+def test_certain_and_impossible_targets():
+    from paper_2605_18643_b200 import zeda
+    T, d, V = 64, 256, 900
+    x, w, target, grad = make(T, d, V, seed=12)
+    # the first tokens' targets nearly certain (likelihoods of 1e-9 and below), the next ones all but impossible
+    scale = torch.ones(T, 1, device=DEV)
+    wt = torch.nn.functional.normalize(w[target.long()].float(), dim=1) * math.sqrt(d)
+    x = x.float()
+    x[:20] = wt[:20] * torch.linspace(1.0, 3.0, 20, device=DEV)[:, None]
+    x[20:40] = -wt[20:40] * torch.linspace(1.0, 3.0, 20, device=DEV)[:, None]
+    x = (x * scale).to(torch.bfloat16)
+    m = zeda.VocabLoss(w, T)
+    nll, lse, gx, gw = check(zeda, m, x, w, target, grad)
+    want = reference(x, w, target, grad)
+    # where the target is nearly certain the likelihood keeps its digits: relative, not to the logits
+    rel = (nll.double() - want[0]).abs()[:20] / want[0][:20]
+    assert bool((rel <= want[2][:20] + 4e-6).all())
+    # a vocabulary of one row: certain, and without gradient
+    one = zeda.VocabLoss(w[:1].contiguous(), T)
+    zero = torch.zeros(T, dtype=torch.int32, device=DEV)
+    nll, lse = one.nll(x, zero)
+    gx, gw = one.backward(x, zero, nll, lse, grad)
+    assert not nll.any() and not gx.any() and not gw.any()
+    m.close()
+    one.close()
+
+
+def test_the_gradient_is_the_likelihoods_difference_quotient():
+    from paper_2605_18643_b200 import zeda
+    T, d, V, h = 96, 128, 600, 2.0 ** -5
+    g = torch.Generator(device=DEV)
+    g.manual_seed(13)
+    x = (torch.randint(-48, 49, (T, d), generator=g, device=DEV) / 16).to(torch.bfloat16)  # x +- h are bf16 numbers too
+    w = (torch.randn(V, d, generator=g, device=DEV) * (0.5 / math.sqrt(d))).to(torch.bfloat16)
+    target = torch.randint(0, V, (T,), generator=g, device=DEV).to(torch.int32)
+    grad = torch.rand(T, generator=g, device=DEV)
+    m = zeda.VocabLoss(w, T)
+    nll, lse, gx, gw = check(zeda, m, x, w, target, grad)
+    v = torch.randint(0, 2, (T, d), generator=g, device=DEV) * 2 - 1
+    up, down = ((x.float() + s * h * v).to(torch.bfloat16) for s in (1, -1))
+    assert torch.equal(up.float() - x.float(), h * v.float())
+    diff = (m.nll(up, target)[0].double() - m.nll(down, target)[0].double()) * grad.double()
+    want = 2 * h * (gx.double() * v).sum(dim=1)
+    r = reference(x, w, target, grad)
+    reach = (h * v.double() @ w.double().t()).abs().amax(dim=1)  # how far a logit moves
+    # third derivative of the log-sum-exp: a third central moment of numbers within +-reach
+    tol = grad.double() * (8 * reach ** 3 / 3 + 2 * r[2]) + 2 * h * r[5].sum(dim=1)
+    assert bool(((diff - want).abs() <= tol).all())
+    assert float(tol.norm()) < 0.5 * float(diff.norm())
+    m.close()
+
+
+def test_no_result_depends_on_the_call_in_front_graphs_and_streams():
+    from paper_2605_18643_b200 import zeda
+    d, V = 256, 3001
+    sets = [make(T, d, V, seed=T, ignored=0.3) for T in (600, 40, 257)]
+    w = sets[0][1]
+    for flags in (0, zeda.FLAG_NO_DEPENDENT_LAUNCH):
+        m = zeda.VocabLoss(w, 600, flags=flags)
+
+        def step(x, _, target, grad):
+            nll, lse = m.nll(x, target)
+            return (nll, lse) + m.backward(x, target, nll, lse, grad)
+
+        alone = []
+        for s in sets:
+            alone.append([t.clone() for t in step(*s)])
+            torch.cuda.synchronize()
+        for _ in range(3):
+            for got, want in zip([step(*s) for s in sets], alone):
+                assert all(torch.equal(a, b) for a, b in zip(got, want))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            got = step(*sets[2])
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, alone[2]))
+        x, _, target, grad = (t.clone() for t in sets[2])
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs = step(x, None, target, grad)
+        for src in (sets[2], [t[:257].contiguous() for t in sets[0]], sets[2]):
+            x.copy_(src[0]); target.copy_(src[2]); grad.copy_(src[3])
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(outs, step(*src)))
+        # new values of the same matrix
+        keep = w.clone()
+        w.mul_(0.5)
+        check(zeda, m, sets[1][0], w, sets[1][2], sets[1][3])
+        w.copy_(keep)
+        m.check()
+        m.close()
+
+
+def test_refusals():
+    from paper_2605_18643_b200 import zeda
+    x, w, target, grad = make(16, 128, 300, seed=14)
+    for bad in (dict(max_tokens=0), dict(max_tokens=2 ** 20 + 1), dict(flags=3)):
+        kw = dict(max_tokens=16)
+        kw.update(bad)
+        with pytest.raises(zeda.ZedaError):
+            zeda.VocabLoss(w, **kw)
+    with pytest.raises(zeda.ZedaError):
+        zeda.VocabLoss(torch.zeros((8, 96), dtype=torch.bfloat16, device=DEV), 16)
+    with pytest.raises(zeda.ZedaError) as e:
+        zeda.VocabLoss(w, 16, workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
+    assert e.value.status == zeda.ERR_WORKSPACE
+    m = zeda.VocabLoss(w, 16, backward=False)
+    nll, lse = m.nll(x, target)
+    with pytest.raises(zeda.ZedaError):
+        m.backward(x, target, nll, lse, grad)
+    x17, _, t17, _ = make(17, 128, 300, seed=15)
+    with pytest.raises(zeda.ZedaError):
+        m.nll(x17, t17)
+    odd = torch.empty(16 * 128 + 1, dtype=torch.bfloat16, device=DEV)[1:].view(16, 128)
+    with pytest.raises(zeda.ZedaError):
+        m.nll(odd, target)
+    m.close()
+    m = zeda.VocabLoss(w, 16)
+    for kw in (dict(grad_x=x), dict(grad_w=w)):
+        with pytest.raises(zeda.ZedaError) as e:
+            m.backward(x, target, nll, lse, grad, **kw)
+        assert "overlap" in str(e.value)
+    m.check()
+    m.close()

@@ -1,0 +1,52 @@
+"""Argument checks of the training-objective calls that need no device."""
+import ctypes
+
+import pytest
+
+from paper_2605_18643_b200 import build
+
+build.build_library()
+from paper_2605_18643_b200 import zeda  # noqa: E402
+
+
+def test_calls_without_a_handle_are_refused():
+    b = zeda.Balance(0, 0.1, 2.0)
+    assert zeda.lib.zeda_moe_balance_loss(None, None, None, None, 1, ctypes.byref(b), None, None, None, None, None) == zeda.ERR_INVALID_ARG
+    assert zeda.lib.zeda_moe_router_backward(None, None, None, None, 1, ctypes.byref(b), None, None, None, None, None, None) == zeda.ERR_INVALID_ARG
+    assert zeda.lib.zeda_vocab_nll(None, None, None, 1, None, None, None) == zeda.ERR_INVALID_ARG
+    assert zeda.lib.zeda_vocab_nll_backward(None, None, None, 1, None, None, None, None, None, None) == zeda.ERR_INVALID_ARG
+    assert zeda.lib.zeda_vocab_check(None, None) == zeda.ERR_INVALID_ARG
+    assert zeda.lib.zeda_vocab_destroy(None) == zeda.OK
+
+
+def size(*c):
+    return int(zeda.lib.zeda_vocab_workspace_bytes(ctypes.byref(zeda.VocabConfig(*c))))
+
+
+def test_workspace_of_the_likelihood():
+    d, V, T = 2048, 131072, 8192
+    need = size(d, V, T, 1, 0, 0)
+    assert need % 256 == 0 and need < T * V * 2 / 4           # far below the logits, even in two bytes each
+    assert size(d, V, T, 0, 0, 0) < need and size(d, V, 1, 0, 0, 0) < size(d, V, T, 0, 0, 0)
+    assert size(d, 1, 1, 1, 0, 0) > 0 and size(64, 1 << 24, 1, 0, 0, 4) > 0
+
+
+@pytest.mark.parametrize("c", [
+    (2040, 100, 8, 1, 0, 0), (0, 100, 8, 1, 0, 0), (8256, 100, 8, 1, 0, 0), (64, 0, 8, 1, 0, 0), (64, (1 << 24) + 1, 8, 1, 0, 0),
+    (64, 100, 0, 1, 0, 0), (64, 100, (1 << 20) + 1, 1, 0, 0), (64, 100, 8, 2, 0, 0), (64, 100, 8, 1, 0, 1),
+])
+def test_configurations_that_are_refused(c):
+    assert size(*c) == 0 and zeda.last_error() != ""
+    h = ctypes.c_void_p()
+    st = zeda.lib.zeda_vocab_create(ctypes.byref(zeda.VocabConfig(*c)), None, None, 0, ctypes.byref(h))
+    assert st in (zeda.ERR_INVALID_ARG, zeda.ERR_UNSUPPORTED) and not h.value
+
+
+def test_create_refuses_before_touching_a_device():
+    h = ctypes.c_void_p()
+    cfg = zeda.VocabConfig(64, 100, 8, 1, 0, 0)
+    assert zeda.lib.zeda_vocab_create(ctypes.byref(cfg), None, None, 0, ctypes.byref(h)) == zeda.ERR_INVALID_ARG
+    assert zeda.lib.zeda_vocab_create(ctypes.byref(cfg), ctypes.c_void_p(256), ctypes.c_void_p(256), 256, ctypes.byref(h)) == zeda.ERR_WORKSPACE
+    assert zeda.lib.zeda_vocab_create(ctypes.byref(cfg), ctypes.c_void_p(8), ctypes.c_void_p(256), 1 << 40, ctypes.byref(h)) == zeda.ERR_INVALID_ARG
+    assert zeda.lib.zeda_vocab_create(ctypes.byref(cfg), ctypes.c_void_p(256), ctypes.c_void_p(128), 1 << 40, ctypes.byref(h)) == zeda.ERR_INVALID_ARG
+    assert zeda.lib.zeda_vocab_create(None, None, None, 0, ctypes.byref(h)) == zeda.ERR_INVALID_ARG

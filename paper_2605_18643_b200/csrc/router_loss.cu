@@ -12,8 +12,13 @@
 // of derivative; both gradients end in the same T x (N + N_Z) numbers and are written by one pass.
 //
 // One warp per token, candidate j in lane j % 32, register j / 32, fp32 throughout.  What bounds both kernels is the
-// logits' way through HBM (the losses read them once, the gradient reads and writes them once); small calls are latency.
+// logits' way through HBM (the losses read them once, the gradient reads and writes them once) and, close behind it, the
+// issue of instructions: hence the number of registers per lane as a template parameter of every value (only the last of
+// them needs a bound), and exponentials as ex2 (2^-22 relative; 3 instructions for expf's 8).
+// Small calls are latency.
 #include <cooperative_groups.h>
+
+#include <type_traits>
 
 #include "route_token.cuh"
 
@@ -23,10 +28,14 @@ namespace {
 
 namespace cg = cooperative_groups;
 
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kLossWarps = 16;               // of a CTA of the loss kernel
 constexpr int kLossThreads = 32 * kLossWarps;
-constexpr int kLossCluster = 8;              // CTAs that add up their sums among themselves first
-constexpr int kLossMaxCtas = 144;            // 18 clusters of 8: one CTA per SM
+// CTAs that add up their sums among themselves first.  Pairs always fit: of the 148 SMs, clusters of 4 and 8 leave out
+// the rest of every group of SMs, and the grid takes a second turn (65,536 tokens, 511 candidates: 77 and 88 us).
+constexpr int kLossCluster = 2;
+constexpr int kLossMaxCtas = 148;
+constexpr int kLossOneCta = 128;             // up to so many tokens one CTA does it all
 constexpr int kGradWarps = 8;
 
 // What the losses' slopes are made of, as the kernels take it.
@@ -35,10 +44,12 @@ struct BalanceArgs {
     float alpha, group_w;
 };
 
+// Logits of one token (RPL = candidates / 32 rounded up): -inf beyond the last.
 template <int RPL>
 __device__ __forceinline__ void load_logits(const float *__restrict__ row, int n_cand, int lane, float (&v)[RPL]) {
 #pragma unroll
-    for (int r = 0; r < RPL; ++r) v[r] = ldcg_if(r * 32 + lane < n_cand, row + r * 32 + lane, -INFINITY);
+    for (int r = 0; r + 1 < RPL; ++r) v[r] = __ldcg(row + r * 32 + lane);
+    v[RPL - 1] = ldcg_if((RPL - 1) * 32 + lane < n_cand, row + (RPL - 1) * 32 + lane, -INFINITY);
 }
 
 __device__ __forceinline__ float warp_max(float v) {
@@ -47,8 +58,16 @@ __device__ __forceinline__ float warp_max(float v) {
     return v;
 }
 
-// Softmax of one token in place, p = expf(l - m) * inv.  A token all of whose logits are -inf has probabilities 0; a NaN
-// stays one.
+// exp(l - m), m the token's maximum.  The difference comes first: l log2(e) - m log2(e) in one fused operation would
+// overflow at masks of the type's lowest value.
+__device__ __forceinline__ float exp_above(float l, float m) {
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"((l - m) * kLog2e));
+    return e;
+}
+
+// Softmax of one token: v becomes exp(l - max), the probabilities are v * inv.  A token all of whose logits are -inf has
+// probabilities 0; a NaN stays one.
 template <int RPL>
 __device__ __forceinline__ void softmax_row(float (&v)[RPL], float &m, float &inv) {
     m = v[0];
@@ -59,19 +78,17 @@ __device__ __forceinline__ void softmax_row(float (&v)[RPL], float &m, float &in
     float sum = 0.f;
 #pragma unroll
     for (int r = 0; r < RPL; ++r) {
-        v[r] = expf(v[r] - m);
+        v[r] = exp_above(v[r], m);
         sum += v[r];
     }
     sum = warp_sum(sum);
     inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-    for (int r = 0; r < RPL; ++r) v[r] *= inv;
 }
 
 // Sums over the tokens: probabilities and counts per candidate, tokens that count.  Every warp adds up its tokens in
 // registers, the warps of a CTA through shared memory, the CTAs of a cluster through each other's, each taking a share of
 // the columns; the clusters' sums go to the workspace, and the CTA that finishes last adds those and writes the results.
-// The order of every sum is fixed by T alone.
+// The order of every sum is fixed by T and the device alone.
 template <int RPL>
 __global__ void __launch_bounds__(kLossThreads, 1)
 balance_loss_kernel(const float *__restrict__ logits, const int32_t *__restrict__ topk_idx, const uint8_t *__restrict__ mask, int T,
@@ -96,29 +113,44 @@ balance_loss_kernel(const float *__restrict__ logits, const int32_t *__restrict_
     int my_tokens = 0;
     const int stride = gridDim.x * kLossWarps;
     const int first = blockIdx.x + warp * gridDim.x;  // consecutive tokens to different SMs
-    for (int t = first; t < T; t += 2 * stride) {
-        float v[2][RPL];
-        bool on[2];
+    // two tokens at a time, the next two on their way meanwhile
+    float next[2][RPL];
+    bool next_on[2];
+    int next_id[2];
+    auto fetch = [&](int t) {
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             const int tt = t + n * stride;
-            on[n] = tt < T && (!mask || __ldcg(mask + tt) != 0);
-            if (on[n]) {
-                load_logits<RPL>(logits + (size_t)tt * C, C, lane, v[n]);
-                if (lane < a.K) {
-                    const int id = __ldcg(topk_idx + (size_t)tt * a.K + lane);
-                    if (id >= 0 && id < C) atomicAdd(&hist[id], 1);
-                }
-                ++my_tokens;
+            next_on[n] = tt < T && (!mask || __ldcg(mask + tt) != 0);
+            next_id[n] = -1;
+            if (next_on[n]) {
+                if (lane < a.K) next_id[n] = __ldcg(topk_idx + (size_t)tt * a.K + lane);
+                load_logits<RPL>(logits + (size_t)tt * C, C, lane, next[n]);
             }
         }
+    };
+    fetch(first);
+    for (int t = first; t < T; t += 2 * stride) {
+        float v[2][RPL];
+        bool on[2];
+        int id[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            on[n] = next_on[n];
+            id[n] = next_id[n];
+#pragma unroll
+            for (int r = 0; r < RPL; ++r) v[n][r] = next[n][r];
+        }
+        if (t + 2 * stride < T) fetch(t + 2 * stride);
 #pragma unroll
         for (int n = 0; n < 2; ++n)
             if (on[n]) {
+                ++my_tokens;
+                if (id[n] >= 0 && id[n] < C) atomicAdd(&hist[id[n]], 1);
                 float m, inv;
                 softmax_row<RPL>(v[n], m, inv);
 #pragma unroll
-                for (int r = 0; r < RPL; ++r) acc[r] += v[n][r];
+                for (int r = 0; r < RPL; ++r) acc[r] = fmaf(v[n][r], inv, acc[r]);
             }
     }
 #pragma unroll
@@ -132,41 +164,72 @@ balance_loss_kernel(const float *__restrict__ logits, const int32_t *__restrict_
         for (int w = 0; w < kLossWarps; ++w) s += warp_cols[w * C + j];
         col[j] = s;
     }
-    cg::cluster_group cluster = cg::this_cluster();
-    const int cs = cluster.num_blocks(), cr = cluster.block_rank();
-    const int n_clusters = gridDim.x / cs, cid = blockIdx.x / cs;
-    cluster.sync();
-    // columns 0..C-1, and C for the tokens
-    for (int j = cr * kLossThreads + threadIdx.x; j <= C; j += cs * kLossThreads) {
-        float s = 0.f;
-        int n = 0;
-        const int h = j < C ? j : kMaxCand;
-        for (int r = 0; r < cs; ++r) {
-            if (j < C) s += *cluster.map_shared_rank(&col[j], r);
-            n += *cluster.map_shared_rank(&hist[h], r);
+    const bool alone = gridDim.x == 1;
+    int n_clusters = 1;
+    if (!alone) {
+        cg::cluster_group cluster = cg::this_cluster();
+        const int cs = cluster.num_blocks(), cr = cluster.block_rank();
+        const int cid = blockIdx.x / cs;
+        n_clusters = gridDim.x / cs;
+        cluster.sync();
+        // columns 0..C-1, and C for the tokens
+        for (int j = cr * kLossThreads + threadIdx.x; j <= C; j += cs * kLossThreads) {
+            float s = 0.f;
+            int n = 0;
+            const int h = j < C ? j : kMaxCand;
+            for (int r = 0; r < cs; ++r) {
+                if (j < C) s += *cluster.map_shared_rank(&col[j], r);
+                n += *cluster.map_shared_rank(&hist[h], r);
+            }
+            if (j < C) part[(size_t)cid * C + j] = s;
+            part_counts[(size_t)cid * (C + 1) + j] = n;
         }
-        if (j < C) part[(size_t)cid * C + j] = s;
-        part_counts[(size_t)cid * (C + 1) + j] = n;
+        __threadfence();
+        cluster.sync();  // no CTA leaves while another reads its sums
+        if (threadIdx.x == 0) s_last = atomicInc(reinterpret_cast<unsigned *>(done), gridDim.x - 1) == gridDim.x - 1;  // back at 0 behind the last
+        __syncthreads();
+        if (!s_last) return;
+        __threadfence();
     }
-    cluster.sync();  // no CTA leaves while another reads its sums; also the stores above come before the count below
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) s_last = atomicInc(reinterpret_cast<unsigned *>(done), gridDim.x - 1) == gridDim.x - 1;  // back at 0 behind the last
-    __syncthreads();
-    if (!s_last) return;
-    __threadfence();
 
-    int n = 0;
-    for (int c = 0; c < n_clusters; ++c) n += __ldcg(part_counts + (size_t)c * (C + 1) + C);
+    int n = alone ? hist[kMaxCand] : 0;
+    if (!alone) {  // a lane a cluster
+        for (int c = lane; c < n_clusters; c += 32) n += __ldcg(part_counts + (size_t)c * (C + 1) + C);
+        n = __reduce_add_sync(kFull, n);
+    }
     const double inv_n = n > 0 ? 1.0 / (double)n : 0.0;
     double s4[4] = {0.0, 0.0, 0.0, 0.0};  // vanilla: sum f_i P_i; group: f_E, P_E, and f_Z, P_Z
-    for (int j = threadIdx.x; j < C; j += kLossThreads) {
-        float s = 0.f;
-        int k = 0;
-        for (int c = 0; c < n_clusters; ++c) {
-            s += __ldcg(part + (size_t)c * C + j);
-            k += __ldcg(part_counts + (size_t)c * (C + 1) + j);
+    int32_t *group_counts = reinterpret_cast<int32_t *>(warp_cols) + kLossWarps / 2 * C;
+    constexpr int kBatch = 20;
+    // a warp 32 columns of some of the clusters; the warps' sums meet in shared memory
+    const int blocks = (C + 31) / 32, groups = blocks >= kLossWarps ? 1 : min(kLossWarps / blocks, kLossWarps / 2);
+    if (!alone && warp < blocks * groups) {
+        const int j = warp % blocks * 32 + lane, group = warp / blocks;
+        if (j < C) {
+            float s = 0.f;
+            int k = 0;
+            // many loads in flight: one after the other, 74 clusters took 14 to 26 us
+            for (int c0 = group; c0 < n_clusters; c0 += kBatch * groups) {
+                float ps[kBatch], pc[kBatch];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) {
+                    const int c = c0 + u * groups;
+                    ps[u] = ldcg_if(c < n_clusters, part + (size_t)c * C + j, 0.f);
+                    pc[u] = ldcg_if(c < n_clusters, reinterpret_cast<const float *>(part_counts) + (size_t)c * (C + 1) + j, 0.f);
+                }
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) { s += ps[u]; k += __float_as_int(pc[u]); }
+            }
+            warp_cols[group * C + j] = s;
+            group_counts[group * C + j] = k;
         }
+    }
+    __syncthreads();
+    for (int j = threadIdx.x; j < C; j += kLossThreads) {
+        float s = alone ? col[j] : 0.f;
+        int k = alone ? hist[j] : 0;
+        if (!alone)
+            for (int g = 0; g < groups; ++g) { s += warp_cols[g * C + j]; k += group_counts[g * C + j]; }
         const double f = k * inv_n, P = n > 0 ? s * inv_n : 0.0;
         counts[j] = k;
         if (p_mean) p_mean[j] = (float)P;
@@ -203,28 +266,47 @@ balance_loss_kernel(const float *__restrict__ logits, const int32_t *__restrict_
 
 // Gradient to the logits.  The slopes are taken relative to candidate 0's (the softmax's derivative does not see a
 // constant), so that a group's common slope, or the mean load, costs no digits of the differences that are left.
+// The row is written without the slots' own terms; lane k then writes slot k's candidate again, with its term: the same
+// p, slope and sums, so no bit of the rest changes, and no lane has to look for slots among its registers.
 template <int RPL>
-__global__ void __launch_bounds__(32 * kGradWarps)
+__global__ void __launch_bounds__(32 * kGradWarps, RPL > 8 ? 3 : 4)
 router_backward_kernel(const float *__restrict__ logits, const int32_t *__restrict__ topk_idx, const uint8_t *__restrict__ mask, int T,
                        const BalanceArgs a, int gate_mode, const int32_t *__restrict__ counts, const int32_t *__restrict__ n_tokens,
                        const float *__restrict__ grad_loss, const float *__restrict__ grad_topk_w, float *__restrict__ grad_logits) {
     pdl_launch_dependents();
-    extern __shared__ float slot_rows[];  // [kGradWarps][n_cand]: what the chosen candidates get from the routing weights
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int C = a.n_cand, K = a.K;
-    float *slots = slot_rows + warp * C;
-    for (int j = lane; j < C; j += 32) slots[j] = 0.f;
     pdl_wait();
 
+    // the first token's row comes in while the slopes are made, the next token's while one is worked on
+    const int step = gridDim.x * kGradWarps;
+    float next[RPL];
+    bool next_on = false;
+    int next_id = -1;
+    float next_g = 0.f;
+    auto fetch = [&](int t) {
+        next_on = !mask || __ldcg(mask + t) != 0;
+        if (!next_on) return;
+        if (grad_topk_w && lane < K) {
+            next_id = __ldcg(topk_idx + (size_t)t * K + lane);
+            next_g = __ldcg(grad_topk_w + (size_t)t * K + lane);
+        }
+        load_logits<RPL>(logits + (size_t)t * C, C, lane, next);
+    };
+    const int first = blockIdx.x + warp * gridDim.x;
+    if (first < T) fetch(first);
     float slope[RPL];
+    float per = 0.f;  // vanilla: slope of one count more than candidate 0's; group: slope of the zero experts
+    int c0 = 0;
 #pragma unroll
     for (int r = 0; r < RPL; ++r) slope[r] = 0.f;
+    const bool vanilla = a.kind == ZEDA_BALANCE_VANILLA;
     if (grad_loss) {
         const double n = max(__ldcg(n_tokens), 1);
         const double scale = (double)__ldcg(grad_loss) * a.alpha / a.K / (n * n);
-        if (a.kind == ZEDA_BALANCE_VANILLA) {
-            const int c0 = __ldcg(counts);
-            const float per = (float)(scale * C);
+        if (vanilla) {
+            c0 = __ldcg(counts);
+            per = (float)(scale * C);
 #pragma unroll
             for (int r = 0; r < RPL; ++r)
                 if (r * 32 + lane < C) slope[r] = per * (float)(__ldcg(counts + r * 32 + lane) - c0);
@@ -243,74 +325,71 @@ router_backward_kernel(const float *__restrict__ logits, const int32_t *__restri
                 cZ += __shfl_xor_sync(kFull, cZ, o);
             }
             const double Z = C - a.n_real, w = a.group_w;
-            const float step = (float)(scale * (a.n_real + Z * w) * ((double)cZ / (Z * w) - (double)cE / a.n_real));
+            per = (float)(scale * (a.n_real + Z * w) * ((double)cZ / (Z * w) - (double)cE / a.n_real));
 #pragma unroll
-            for (int r = 0; r < RPL; ++r) slope[r] = r * 32 + lane >= a.n_real ? step : 0.f;
+            for (int r = 0; r < RPL; ++r) slope[r] = r * 32 + lane >= a.n_real ? per : 0.f;
         }  // (without zero experts every slope is the same)
     }
 
-    for (int t = blockIdx.x + warp * gridDim.x; t < T; t += gridDim.x * kGradWarps) {
+    for (int t = first; t < T; t += step) {
         float *out = grad_logits + (size_t)t * C;
-        if (mask && __ldcg(mask + t) == 0) {
+        const float *row = logits + (size_t)t * C;
+        const bool on = next_on;
+        int id = next_id;
+        float e[RPL], g = next_g, lk = -INFINITY, sk = 0.f;
+#pragma unroll
+        for (int r = 0; r < RPL; ++r) e[r] = next[r];
+        if (!on) {
+            if (t + step < T) fetch(t + step);
 #pragma unroll
             for (int r = 0; r < RPL; ++r)
-                if (r * 32 + lane < C) out[r * 32 + lane] = 0.f;
+                if (r + 1 < RPL || r * 32 + lane < C) out[r * 32 + lane] = 0.f;
             continue;
         }
-        const float *row = logits + (size_t)t * C;
-        float p[RPL];
-        load_logits<RPL>(row, C, lane, p);
-        int id = -1;
-        float g = 0.f, lk = -INFINITY;
-        if (grad_topk_w && lane < K) {
-            id = __ldcg(topk_idx + (size_t)t * K + lane);
-            if (id < 0 || id >= C || (gate_mode == ZEDA_GATE_RENORM_REAL && id >= a.n_real)) id = -1;
-            if (id >= 0) {
-                g = __ldcg(grad_topk_w + (size_t)t * K + lane);
-                lk = __ldcg(row + id);
-            }
+        if (id < 0 || id >= C || (gate_mode == ZEDA_GATE_RENORM_REAL && id >= a.n_real)) { id = -1; g = 0.f; }
+        if (id >= 0) {
+            lk = __ldcg(row + id);
+            if (grad_loss) sk = vanilla ? per * (float)(__ldcg(counts + id) - c0) : id >= a.n_real ? per : 0.f;
         }
+        if (t + step < T) fetch(t + step);
         float m, inv;
-        softmax_row<RPL>(p, m, inv);
-        float all = 0.f;  // sum_j p_j s_j
+        softmax_row<RPL>(e, m, inv);
+        float base = 0.f;  // what every candidate's slope is compared with: sum_j p_j s_j, and for the raw softmax sum p_k g_k
         if (grad_loss) {
 #pragma unroll
-            for (int r = 0; r < RPL; ++r) all += r * 32 + lane < C ? p[r] * slope[r] : 0.f;
-            all = warp_sum(all);
+            for (int r = 0; r < RPL; ++r) base = fmaf(e[r], slope[r], base);
+            base = warp_sum(base) * inv;
         }
-        float raw = 0.f;  // raw softmax: sum over the slots of p_k g_k, which every candidate feels
+        float u = 0.f;
         if (grad_topk_w) {
             // the slots' weights: softmax over the chosen logits, or the chosen entries of the softmax over all
-            float u;
             if (gate_mode == ZEDA_GATE_SOFTMAX_RAW) {
-                u = id >= 0 ? expf(lk - m) * inv * g : 0.f;
-                raw = warp_sum(u);
+                u = id >= 0 ? exp_above(lk, m) * inv * g : 0.f;
+                base += warp_sum(u);
             } else {
                 float mk = warp_max(lk);
                 if (mk == -INFINITY) mk = 0.f;
-                const float e = id >= 0 ? expf(lk - mk) : 0.f;
-                const float sum = warp_sum(e);
-                const float w = sum == 0.f ? 0.f : e / sum;
+                const float x = id >= 0 ? exp_above(lk, mk) : 0.f;
+                const float sum = warp_sum(x);
+                const float w = sum == 0.f ? 0.f : x / sum;
                 u = w * (g - warp_sum(w * g));
-            }
-            // one slot after the other, each by the lane that owns its column: an id that comes twice gets both
-            for (int k = 0; k < K; ++k) {
-                const int idk = __shfl_sync(kFull, id, k);
-                const float uk = __shfl_sync(kFull, u, k);
-                if (idk >= 0 && lane == (idk & 31)) slots[idk] += uk;
             }
         }
 #pragma unroll
-        for (int r = 0; r < RPL; ++r) {
-            const int j = r * 32 + lane;
-            if (j < C) {
-                float d = p[r] * (slope[r] - all - raw);
-                if (grad_topk_w) {
-                    d += slots[j];
-                    slots[j] = 0.f;
+        for (int r = 0; r < RPL; ++r)
+            if (r + 1 < RPL || r * 32 + lane < C) out[r * 32 + lane] = e[r] * inv * (slope[r] - base);
+        if (grad_topk_w) {
+            const unsigned same = __match_any_sync(kFull, id);  // the slots of this id
+            if (__any_sync(kFull, id >= 0 && (same & (same - 1)) != 0)) {  // an id that comes twice gets all its slots, in their order
+                float all = 0.f;
+                for (int k = 0; k < K; ++k) {
+                    const float uk = __shfl_sync(kFull, u, k);
+                    if (same >> k & 1u) all += uk;
                 }
-                out[j] = d;
+                u = all;
             }
+            __syncwarp();  // the row's stores come first
+            if (id >= 0 && lane == __ffs(same) - 1) out[id] = exp_above(lk, m) * inv * (sk - base) + u;
         }
     }
 }
@@ -350,15 +429,14 @@ zeda_status_t on_device(zeda_moe *h) {
 template <int RPL>
 cudaError_t launch_balance(const zeda_moe *h, const float *logits, const int32_t *topk_idx, const uint8_t *mask, int T,
                            const BalanceArgs &a, float *loss, int32_t *counts, float *p_mean, int32_t *n_tokens, cudaStream_t s) {
-    // a CTA for 32 tokens, in whole clusters
-    int ctas = (T + 2 * kLossWarps - 1) / (2 * kLossWarps);
+    // one CTA, or a CTA for 32 tokens, in whole clusters
+    int ctas = T <= kLossOneCta ? 1 : (T + 2 * kLossWarps - 1) / (2 * kLossWarps);
+    if (ctas > h->sm_count) ctas = h->sm_count;
     if (ctas > kLossMaxCtas) ctas = kLossMaxCtas;
-    int cs = kLossCluster;
-    while (cs > ctas) cs /= 2;
+    const int cs = ctas == 1 ? 1 : kLossCluster;
     ctas = ctas / cs * cs;
-    const int max_clusters = kLossMaxCtas / kLossCluster;
     float *part = h->ws.stat_part;
-    int32_t *part_counts = reinterpret_cast<int32_t *>(part + (size_t)max_clusters * a.n_cand);
+    int32_t *part_counts = reinterpret_cast<int32_t *>(part + (size_t)(kLossMaxCtas / kLossCluster) * a.n_cand);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ctas);
     cfg.blockDim = dim3(kLossThreads);
@@ -381,23 +459,27 @@ cudaError_t launch_backward(const zeda_moe *h, const float *logits, const int32_
                             const BalanceArgs &a, const int32_t *counts, const int32_t *n_tokens, const float *grad_loss,
                             const float *grad_topk_w, float *grad_logits, cudaStream_t s) {
     int ctas = (T + kGradWarps - 1) / kGradWarps;
-    const int most = h->sm_count * 4;
+    const int most = h->sm_count * (RPL > 8 ? 3 : 4);
     if (ctas > most) ctas = most;
-    return launch_kernel(h->pdl, router_backward_kernel<RPL>, dim3(ctas), dim3(32 * kGradWarps),
-                         (size_t)kGradWarps * a.n_cand * sizeof(float), s, logits, topk_idx, mask, T, a, (int)h->cfg.gate_mode, counts,
-                         n_tokens, grad_loss, grad_topk_w, grad_logits);
+    return launch_kernel(h->pdl, router_backward_kernel<RPL>, dim3(ctas), dim3(32 * kGradWarps), 0, s, logits, topk_idx, mask, T, a,
+                         (int)h->cfg.gate_mode, counts, n_tokens, grad_loss, grad_topk_w, grad_logits);
+}
+
+// fn(integral constant RPL) for the candidates / 32, rounded up
+template <typename F>
+cudaError_t by_registers(int n_cand, F &&fn) {
+    static_assert(kMaxCand == 512, "16 registers a lane");
+    switch ((n_cand + 31) / 32) {
+#define ZEDA_RPL_CASE(R) case R: return fn(std::integral_constant<int, R>{});
+        ZEDA_RPL_CASE(1) ZEDA_RPL_CASE(2) ZEDA_RPL_CASE(3) ZEDA_RPL_CASE(4) ZEDA_RPL_CASE(5) ZEDA_RPL_CASE(6) ZEDA_RPL_CASE(7)
+        ZEDA_RPL_CASE(8) ZEDA_RPL_CASE(9) ZEDA_RPL_CASE(10) ZEDA_RPL_CASE(11) ZEDA_RPL_CASE(12) ZEDA_RPL_CASE(13) ZEDA_RPL_CASE(14)
+        ZEDA_RPL_CASE(15)
+        default: return fn(std::integral_constant<int, 16>{});
+#undef ZEDA_RPL_CASE
+    }
 }
 
 }  // namespace
-
-#define ZEDA_LOSS_DISPATCH(CALL, ...)                   \
-    (a.n_cand <= 32    ? CALL<1>(__VA_ARGS__)           \
-     : a.n_cand <= 64  ? CALL<2>(__VA_ARGS__)           \
-     : a.n_cand <= 96  ? CALL<3>(__VA_ARGS__)           \
-     : a.n_cand <= 128 ? CALL<4>(__VA_ARGS__)           \
-     : a.n_cand <= 192 ? CALL<6>(__VA_ARGS__)           \
-     : a.n_cand <= 256 ? CALL<8>(__VA_ARGS__)           \
-                       : CALL<16>(__VA_ARGS__))
 
 }  // namespace zeda
 
@@ -419,8 +501,10 @@ extern "C" zeda_status_t zeda_moe_balance_loss(zeda_moe_t *h, const float *logit
     }
     if ((st = on_device(h)) != ZEDA_OK) return st;
     const BalanceArgs a = balance_args(h, balance);
-    const cudaError_t e = ZEDA_LOSS_DISPATCH(launch_balance, h, logits, topk_idx, token_mask, T, a, loss, counts, p_mean, n_tokens,
-                                             static_cast<cudaStream_t>(stream));
+    const cudaError_t e = by_registers(a.n_cand, [&](auto rpl) {
+        return launch_balance<decltype(rpl)::value>(h, logits, topk_idx, token_mask, T, a, loss, counts, p_mean, n_tokens,
+                                                    static_cast<cudaStream_t>(stream));
+    });
     if (e != cudaSuccess) { set_error("balance loss launch: %s", cudaGetErrorString(e)); return ZEDA_ERR_CUDA; }
     h->last_launches = 1;
     return ZEDA_OK;
@@ -449,8 +533,10 @@ extern "C" zeda_status_t zeda_moe_router_backward(zeda_moe_t *h, const float *lo
     const char *lb = reinterpret_cast<const char *>(logits), *gb = reinterpret_cast<const char *>(grad_logits);
     if (lb < gb + bytes && gb < lb + bytes) { set_error("logits and grad_logits overlap"); return ZEDA_ERR_INVALID_ARG; }
     if ((st = on_device(h)) != ZEDA_OK) return st;
-    const cudaError_t e = ZEDA_LOSS_DISPATCH(launch_backward, h, logits, topk_idx, token_mask, T, a, counts, n_tokens, grad_loss,
-                                             grad_topk_w, grad_logits, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = by_registers(a.n_cand, [&](auto rpl) {
+        return launch_backward<decltype(rpl)::value>(h, logits, topk_idx, token_mask, T, a, counts, n_tokens, grad_loss, grad_topk_w,
+                                                     grad_logits, static_cast<cudaStream_t>(stream));
+    });
     if (e != cudaSuccess) { set_error("router backward launch: %s", cudaGetErrorString(e)); return ZEDA_ERR_CUDA; }
     h->last_launches = 1;
     return ZEDA_OK;

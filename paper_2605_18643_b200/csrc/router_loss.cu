@@ -52,38 +52,59 @@ __device__ __forceinline__ void load_logits(const float *__restrict__ row, int n
     v[RPL - 1] = ldcg_if((RPL - 1) * 32 + lane < n_cand, row + (RPL - 1) * 32 + lane, -INFINITY);
 }
 
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, o));
-    return v;
+__device__ __forceinline__ float warp_max(float v) {  // (a NaN is passed over, as by fmaxf)
+    float m;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+    return m;
 }
 
-// exp(l - m), m the token's maximum.  The difference comes first: l log2(e) - m log2(e) in one fused operation would
-// overflow at masks of the type's lowest value.
-__device__ __forceinline__ float exp_above(float l, float m) {
+// Sums over the warp of several values at a time: their shuffles overlap.
+template <int N>
+__device__ __forceinline__ void warp_sums(float (&v)[N]) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(kFull, v[i], o);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
     float e;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"((l - m) * kLog2e));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
     return e;
 }
 
-// Softmax of one token: v becomes exp(l - max), the probabilities are v * inv.  A token all of whose logits are -inf has
-// probabilities 0; a NaN stays one.
+// exp(l - m), m the maximum
+__device__ __forceinline__ float exp_above(float l, float m) { return exp2_fast((l - m) * kLog2e); }
+
+// The numerators of a token's softmax: v becomes exp(l - max), m the maximum (0 if every logit is -inf: the numerators are
+// 0 then, and so is what is made of them).  A NaN stays one.  In units of ln 2 a fused multiply-add does for subtraction and
+// product; beyond 10^38, where masks of the type's lowest value lie, the product would overflow: there the difference comes first.
 template <int RPL>
-__device__ __forceinline__ void softmax_row(float (&v)[RPL], float &m, float &inv) {
+__device__ __forceinline__ void softmax_numerators(float (&v)[RPL], float &m) {
     m = v[0];
 #pragma unroll
     for (int r = 1; r < RPL; ++r) m = fmaxf(m, v[r]);
     m = warp_max(m);
-    if (m == -INFINITY) m = 0.f;
-    float sum = 0.f;
+    float m2 = m * kLog2e;
+    if (!(fabsf(m) < 1e38f)) {
+        if (m == -INFINITY) m = 0.f;
+        m2 = 0.f;
 #pragma unroll
-    for (int r = 0; r < RPL; ++r) {
-        v[r] = exp_above(v[r], m);
-        sum += v[r];
+        for (int r = 0; r < RPL; ++r) v[r] -= m;
     }
-    sum = warp_sum(sum);
-    inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int r = 0; r < RPL; ++r) v[r] = exp2_fast(fmaf(v[r], kLog2e, -m2));
 }
+
+template <int RPL>
+__device__ __forceinline__ float lane_sum(const float (&v)[RPL]) {
+    float s[2] = {v[0], 0.f};
+#pragma unroll
+    for (int r = 1; r < RPL; ++r) s[r & 1] += v[r];
+    return s[0] + s[1];
+}
+
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
 
 // Sums over the tokens: probabilities and counts per candidate, tokens that count.  Every warp adds up its tokens in
 // registers, the warps of a CTA through shared memory, the CTAs of a cluster through each other's, each taking a share of
@@ -139,19 +160,24 @@ balance_loss_kernel(const float *__restrict__ logits, const int32_t *__restrict_
             on[n] = next_on[n];
             id[n] = next_id[n];
 #pragma unroll
-            for (int r = 0; r < RPL; ++r) v[n][r] = next[n][r];
+            for (int r = 0; r < RPL; ++r) v[n][r] = on[n] ? next[n][r] : -INFINITY;
         }
         if (t + 2 * stride < T) fetch(t + 2 * stride);
+        float m[2], sum[2];
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-            if (on[n]) {
-                ++my_tokens;
-                if (id[n] >= 0 && id[n] < C) atomicAdd(&hist[id[n]], 1);
-                float m, inv;
-                softmax_row<RPL>(v[n], m, inv);
+        for (int n = 0; n < 2; ++n) {  // a token that does not count has numerators 0
+            if (on[n]) ++my_tokens;
+            if (id[n] >= 0 && id[n] < C) atomicAdd(&hist[id[n]], 1);
+            softmax_numerators<RPL>(v[n], m[n]);
+            sum[n] = lane_sum<RPL>(v[n]);
+        }
+        warp_sums<2>(sum);
 #pragma unroll
-                for (int r = 0; r < RPL; ++r) acc[r] = fmaf(v[n][r], inv, acc[r]);
-            }
+        for (int n = 0; n < 2; ++n) {
+            const float inv = inverse(sum[n]);
+#pragma unroll
+            for (int r = 0; r < RPL; ++r) acc[r] = fmaf(v[n][r], inv, acc[r]);
+        }
     }
 #pragma unroll
     for (int r = 0; r < RPL; ++r)
@@ -265,122 +291,125 @@ balance_loss_kernel(const float *__restrict__ logits, const int32_t *__restrict_
 }
 
 // Gradient to the logits.  The slopes are taken relative to candidate 0's (the softmax's derivative does not see a
-// constant), so that a group's common slope, or the mean load, costs no digits of the differences that are left.
-// The row is written without the slots' own terms; lane k then writes slot k's candidate again, with its term: the same
-// p, slope and sums, so no bit of the rest changes, and no lane has to look for slots among its registers.
+// constant), so that a group's common slope, or the mean load, costs no digits of the differences that are left; each CTA
+// keeps them in shared memory.
+// The row is written without the slots' own terms; lane k then writes slot k's candidate again, with its term: no lane has
+// to look for slots among its registers.  A token's row and its slots' logits are on their way while the token in front is
+// worked on, the ids that say where those lie one token earlier still.
 template <int RPL>
-__global__ void __launch_bounds__(32 * kGradWarps, RPL > 8 ? 3 : 4)
+__global__ void __launch_bounds__(32 * kGradWarps, 4)
 router_backward_kernel(const float *__restrict__ logits, const int32_t *__restrict__ topk_idx, const uint8_t *__restrict__ mask, int T,
                        const BalanceArgs a, int gate_mode, const int32_t *__restrict__ counts, const int32_t *__restrict__ n_tokens,
                        const float *__restrict__ grad_loss, const float *__restrict__ grad_topk_w, float *__restrict__ grad_logits) {
     pdl_launch_dependents();
+    __shared__ float slope[RPL * 32];
+    __shared__ int s_load[2];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int C = a.n_cand, K = a.K;
+    if (threadIdx.x < 2) s_load[threadIdx.x] = 0;
+    __syncthreads();
     pdl_wait();
 
-    // the first token's row comes in while the slopes are made, the next token's while one is worked on
-    const int step = gridDim.x * kGradWarps;
-    float next[RPL];
+    const int stride = gridDim.x * kGradWarps;
+    const int first = blockIdx.x + warp * gridDim.x;
+    const bool renorm = gate_mode == ZEDA_GATE_RENORM_REAL, raw = gate_mode == ZEDA_GATE_SOFTMAX_RAW;
+    // the slot of this lane, of token t: its candidate, or -1
+    auto slot_of = [&](int t) {
+        if (!grad_topk_w || lane >= K || t >= T) return -1;
+        const int id = __ldcg(topk_idx + (size_t)t * K + lane);
+        return id < 0 || id >= C || (renorm && id >= a.n_real) ? -1 : id;
+    };
+    float next[RPL], next_g = 0.f, next_lk = -INFINITY;
     bool next_on = false;
-    int next_id = -1;
-    float next_g = 0.f;
-    auto fetch = [&](int t) {
-        next_on = !mask || __ldcg(mask + t) != 0;
+    auto fetch = [&](int t, int id) {
+        next_on = t < T && (!mask || __ldcg(mask + t) != 0);
+        next_g = 0.f;
+        next_lk = -INFINITY;
         if (!next_on) return;
-        if (grad_topk_w && lane < K) {
-            next_id = __ldcg(topk_idx + (size_t)t * K + lane);
+        const float *row = logits + (size_t)t * C;
+        load_logits<RPL>(row, C, lane, next);
+        if (id >= 0) {
+            next_lk = __ldcg(row + id);
             next_g = __ldcg(grad_topk_w + (size_t)t * K + lane);
         }
-        load_logits<RPL>(logits + (size_t)t * C, C, lane, next);
     };
-    const int first = blockIdx.x + warp * gridDim.x;
-    if (first < T) fetch(first);
-    float slope[RPL];
-    float per = 0.f;  // vanilla: slope of one count more than candidate 0's; group: slope of the zero experts
-    int c0 = 0;
-#pragma unroll
-    for (int r = 0; r < RPL; ++r) slope[r] = 0.f;
-    const bool vanilla = a.kind == ZEDA_BALANCE_VANILLA;
+    int id = slot_of(first), next_id = slot_of(first + stride);
+    fetch(first, id);
+
     if (grad_loss) {
         const double n = max(__ldcg(n_tokens), 1);
         const double scale = (double)__ldcg(grad_loss) * a.alpha / a.K / (n * n);
-        if (vanilla) {
-            c0 = __ldcg(counts);
-            per = (float)(scale * C);
-#pragma unroll
-            for (int r = 0; r < RPL; ++r)
-                if (r * 32 + lane < C) slope[r] = per * (float)(__ldcg(counts + r * 32 + lane) - c0);
-        } else if (C > a.n_real) {
-            long long cE = 0, cZ = 0;
-#pragma unroll
-            for (int r = 0; r < RPL; ++r) {
-                const int j = r * 32 + lane;
-                const int c = j < C ? __ldcg(counts + j) : 0;
-                if (j < a.n_real) cE += c;
-                else cZ += c;
+        if (a.kind == ZEDA_BALANCE_VANILLA) {
+            const int c0 = __ldcg(counts);
+            const float per = (float)(scale * C);
+            for (int j = threadIdx.x; j < RPL * 32; j += 32 * kGradWarps) slope[j] = j < C ? per * (float)(__ldcg(counts + j) - c0) : 0.f;
+        } else {
+            int c[2] = {0, 0};
+            for (int j = threadIdx.x; j < C; j += 32 * kGradWarps) c[j >= a.n_real] += __ldcg(counts + j);
+            for (int i = 0; i < 2; ++i) {
+                c[i] = __reduce_add_sync(kFull, c[i]);
+                if (lane == 0) atomicAdd(&s_load[i], c[i]);
             }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                cE += __shfl_xor_sync(kFull, cE, o);
-                cZ += __shfl_xor_sync(kFull, cZ, o);
-            }
-            const double Z = C - a.n_real, w = a.group_w;
-            per = (float)(scale * (a.n_real + Z * w) * ((double)cZ / (Z * w) - (double)cE / a.n_real));
-#pragma unroll
-            for (int r = 0; r < RPL; ++r) slope[r] = r * 32 + lane >= a.n_real ? per : 0.f;
-        }  // (without zero experts every slope is the same)
+            __syncthreads();
+            const double Z = C - a.n_real, w = a.group_w;  // (without zero experts every slope is the same)
+            const float step = Z > 0 ? (float)(scale * (a.n_real + Z * w) * ((double)s_load[1] / (Z * w) - (double)s_load[0] / a.n_real)) : 0.f;
+            for (int j = threadIdx.x; j < RPL * 32; j += 32 * kGradWarps) slope[j] = j >= a.n_real ? step : 0.f;
+        }
+    } else {
+        for (int j = threadIdx.x; j < RPL * 32; j += 32 * kGradWarps) slope[j] = 0.f;
     }
+    __syncthreads();
 
-    for (int t = first; t < T; t += step) {
+    for (int t = first; t < T; t += stride) {
         float *out = grad_logits + (size_t)t * C;
-        const float *row = logits + (size_t)t * C;
         const bool on = next_on;
-        int id = next_id;
-        float e[RPL], g = next_g, lk = -INFINITY, sk = 0.f;
+        const int my_id = id;
+        float e[RPL];
+        const float g = next_g, lk = next_lk;
 #pragma unroll
         for (int r = 0; r < RPL; ++r) e[r] = next[r];
+        id = next_id;
+        fetch(t + stride, id);
+        next_id = slot_of(t + 2 * stride);
         if (!on) {
-            if (t + step < T) fetch(t + step);
 #pragma unroll
             for (int r = 0; r < RPL; ++r)
                 if (r + 1 < RPL || r * 32 + lane < C) out[r * 32 + lane] = 0.f;
             continue;
         }
-        if (id < 0 || id >= C || (gate_mode == ZEDA_GATE_RENORM_REAL && id >= a.n_real)) { id = -1; g = 0.f; }
-        if (id >= 0) {
-            lk = __ldcg(row + id);
-            if (grad_loss) sk = vanilla ? per * (float)(__ldcg(counts + id) - c0) : id >= a.n_real ? per : 0.f;
-        }
-        if (t + step < T) fetch(t + step);
-        float m, inv;
-        softmax_row<RPL>(e, m, inv);
-        float base = 0.f;  // what every candidate's slope is compared with: sum_j p_j s_j, and for the raw softmax sum p_k g_k
-        if (grad_loss) {
-#pragma unroll
-            for (int r = 0; r < RPL; ++r) base = fmaf(e[r], slope[r], base);
-            base = warp_sum(base) * inv;
-        }
-        float u = 0.f;
+        float m;
+        softmax_numerators<RPL>(e, m);
+        // over the warp: the numerators, the same times the slopes; the slots' numerators (of the softmax over the chosen
+        // logits; the raw softmax has them already), the same times their gradients
+        float x = 0.f;
         if (grad_topk_w) {
-            // the slots' weights: softmax over the chosen logits, or the chosen entries of the softmax over all
-            if (gate_mode == ZEDA_GATE_SOFTMAX_RAW) {
-                u = id >= 0 ? exp_above(lk, m) * inv * g : 0.f;
-                base += warp_sum(u);
-            } else {
-                float mk = warp_max(lk);
+            float mk = m;
+            if (!raw) {
+                mk = warp_max(lk);
                 if (mk == -INFINITY) mk = 0.f;
-                const float x = id >= 0 ? exp_above(lk, mk) : 0.f;
-                const float sum = warp_sum(x);
-                const float w = sum == 0.f ? 0.f : x / sum;
-                u = w * (g - warp_sum(w * g));
             }
+            x = my_id >= 0 ? exp_above(lk, mk) : 0.f;
+        }
+        float sums[4] = {lane_sum<RPL>(e), 0.f, x, x * g};
+#pragma unroll
+        for (int r = 0; r < RPL; ++r) sums[1] = fmaf(e[r], slope[r * 32 + lane], sums[1]);
+        warp_sums<4>(sums);
+        const float inv = inverse(sums[0]);
+        float base = sums[1] * inv;  // what every candidate's slope is compared with: sum_j p_j s_j, and for the raw softmax sum p_k g_k
+        float u;
+        if (raw) {
+            u = x * inv * g;
+            base = fmaf(sums[3], inv, base);
+        } else {
+            const float inv_k = inverse(sums[2]);
+            u = x * inv_k * (g - sums[3] * inv_k);
         }
 #pragma unroll
         for (int r = 0; r < RPL; ++r)
-            if (r + 1 < RPL || r * 32 + lane < C) out[r * 32 + lane] = e[r] * inv * (slope[r] - base);
+            if (r + 1 < RPL || r * 32 + lane < C) out[r * 32 + lane] = e[r] * inv * (slope[r * 32 + lane] - base);
         if (grad_topk_w) {
-            const unsigned same = __match_any_sync(kFull, id);  // the slots of this id
-            if (__any_sync(kFull, id >= 0 && (same & (same - 1)) != 0)) {  // an id that comes twice gets all its slots, in their order
+            const unsigned same = __match_any_sync(kFull, my_id);  // the slots of this id
+            if (__any_sync(kFull, my_id >= 0 && (same & (same - 1)) != 0)) {  // an id that comes twice gets all its slots, in their order
                 float all = 0.f;
                 for (int k = 0; k < K; ++k) {
                     const float uk = __shfl_sync(kFull, u, k);
@@ -389,7 +418,7 @@ router_backward_kernel(const float *__restrict__ logits, const int32_t *__restri
                 u = all;
             }
             __syncwarp();  // the row's stores come first
-            if (id >= 0 && lane == __ffs(same) - 1) out[id] = exp_above(lk, m) * inv * (sk - base) + u;
+            if (my_id >= 0 && lane == __ffs(same) - 1) out[my_id] = exp_above(lk, m) * inv * (slope[my_id] - base) + u;
         }
     }
 }
@@ -459,7 +488,7 @@ cudaError_t launch_backward(const zeda_moe *h, const float *logits, const int32_
                             const BalanceArgs &a, const int32_t *counts, const int32_t *n_tokens, const float *grad_loss,
                             const float *grad_topk_w, float *grad_logits, cudaStream_t s) {
     int ctas = (T + kGradWarps - 1) / kGradWarps;
-    const int most = h->sm_count * (RPL > 8 ? 3 : 4);
+    const int most = h->sm_count * 4;
     if (ctas > most) ctas = most;
     return launch_kernel(h->pdl, router_backward_kernel<RPL>, dim3(ctas), dim3(32 * kGradWarps), 0, s, logits, topk_idx, mask, T, a,
                          (int)h->cfg.gate_mode, counts, n_tokens, grad_loss, grad_topk_w, grad_logits);

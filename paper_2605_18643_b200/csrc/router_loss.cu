@@ -297,7 +297,7 @@ balance_loss_kernel(const float *__restrict__ logits, const int32_t *__restrict_
 // to look for slots among its registers.  A token's row and its slots' logits are on their way while the token in front is
 // worked on, the ids that say where those lie one token earlier still.
 template <int RPL>
-__global__ void __launch_bounds__(32 * kGradWarps, 4)
+__global__ void __launch_bounds__(32 * kGradWarps, RPL > 12 ? 3 : 4)
 router_backward_kernel(const float *__restrict__ logits, const int32_t *__restrict__ topk_idx, const uint8_t *__restrict__ mask, int T,
                        const BalanceArgs a, int gate_mode, const int32_t *__restrict__ counts, const int32_t *__restrict__ n_tokens,
                        const float *__restrict__ grad_loss, const float *__restrict__ grad_topk_w, float *__restrict__ grad_logits) {
@@ -488,7 +488,7 @@ cudaError_t launch_backward(const zeda_moe *h, const float *logits, const int32_
                             const BalanceArgs &a, const int32_t *counts, const int32_t *n_tokens, const float *grad_loss,
                             const float *grad_topk_w, float *grad_logits, cudaStream_t s) {
     int ctas = (T + kGradWarps - 1) / kGradWarps;
-    const int most = h->sm_count * 4;
+    const int most = h->sm_count * (RPL > 12 ? 3 : 4);
     if (ctas > most) ctas = most;
     return launch_kernel(h->pdl, router_backward_kernel<RPL>, dim3(ctas), dim3(32 * kGradWarps), 0, s, logits, topk_idx, mask, T, a,
                          (int)h->cfg.gate_mode, counts, n_tokens, grad_loss, grad_topk_w, grad_logits);

@@ -35,7 +35,8 @@ struct zeda_vocab {
     // workspace
     int32_t *meta, *row_token, *row_target;
     float *row_label, *row_lse2, *row_g, *row_gl;
-    float2 *part;
+    float2 *part;  // [rows][part_ld]: a token's partial results side by side
+    int part_ld;
     __nv_bfloat16 *xc, *g;
     float *dx;
     void *maps;    // host-side tensor maps (owned)
@@ -58,15 +59,18 @@ constexpr int kGemmSmem = kStages * kStageBytes + 8 * kStoreBytes + 1024;
 constexpr int kRowThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr size_t kPieceBytes = (size_t)256 << 20;  // of dl at a time
+constexpr int kMaxClusters = 80;                 // CTA pairs of a launch
 constexpr int kMaxSplits = 16;                   // of the vocabulary axis of grad_x
 
-enum VocabMeta { kLive = 0, kVocabError = 1, kVocabMetaCount = 64 };
+enum VocabMeta { kLive = 0, kVocabError = 1, kNextBlock = 2, kVocabMetaCount = 64 };
 
 enum { kModeNll = 0, kModeDl = 1, kModeGrads = 2 };
 
 struct VocabMaps {
-    CUtensorMap x_k, w_k, g_k;     // reduction axis innermost: [rows][k], box {64, 128}
-    CUtensorMap x_mn, w_mn, g_mn;  // reduction axis outermost: (64 elements, k, block of 64), box {64, 64, 2}
+    CUtensorMap x_k, g_k;          // reduction axis innermost: [rows][k], box {64, 128}
+    CUtensorMap w_k[3];            // the same with boxes of 128, 64 and 32 rows: half a block's columns are a multiple of 32
+    CUtensorMap g_mn;              // reduction axis outermost: (64 elements, k, block of 64), box {64, 64, 2}
+    CUtensorMap x_mn, w_mn;        // [k][columns], box {64, 64}
     CUtensorMap g_store;           // [rows][piece], box {64, 32}
     CUtensorMap dx_store;          // [dx_rows][d] fp32, box {32, 32}
 };
@@ -77,7 +81,6 @@ struct GemmArgs {
     int splits;      // slices of the piece that grad_x is summed in
     int dx_pitch;    // rows between two slices' sums
     int first;       // first piece: the sums start here
-    const int32_t *meta_live;
     int32_t *meta;
     const int32_t *row_target;
     float *row_label;
@@ -86,52 +89,112 @@ struct GemmArgs {
     int part_ld;
 };
 
-// A block of outputs: where its operands start and how many steps of the reduction axis it takes.
+// A block of outputs: 256 rows, up to 256 columns, and the steps of the reduction axis that it takes.
 struct Block {
-    int m, n;        // row block / column block
+    int m;           // row block
+    int n, c0, cols; // column block: its number, first column and width (a multiple of 64)
     int k0, ks;      // first step and steps
     int slice;       // grad_x: slice of the piece; -1: grad_w
 };
 
+// `units` blocks of 64 columns cut into `n` parts whose widths differ by at most one unit
+__device__ __forceinline__ void cut_columns(Block &b, int units, int n) {
+    const int u0 = (int)((long long)units * b.n / n), u1 = (int)((long long)units * (b.n + 1) / n);
+    b.c0 = 64 * u0;
+    b.cols = 64 * (u1 - u0);
+}
+
+// Column blocks of the logits: as many as do not lengthen the longest cluster's list of full-sized ones (65,536 rows of
+// the matrix and one row block on 74 clusters: 296 blocks of 192 or 256 columns, not 256 of 256, so that each cluster
+// gets four and as many bytes as the next).
+__host__ __device__ inline int logit_blocks(int kp, int n_rb, int n_clusters) {
+    const int units = (kp + 63) / 64, full = (units + 3) / 4;
+    if (n_rb == 0) return full;
+    const long long turns = ((long long)full * n_rb + n_clusters - 1) / n_clusters;
+    const long long n = turns * n_clusters / n_rb;
+    return n > units ? units : (int)n;
+}
+
+struct Plan {  // of one launch
+    int n_live, n_rb, n_vt, dt, n_blocks;
+};
+
 template <int MODE>
-__device__ __forceinline__ int block_count(const GemmArgs &a, int n_rb) {
-    const int n_vt = (a.kp + kTile - 1) / kTile;
-    if (MODE != kModeGrads) return n_rb * n_vt;
-    const int dt = (a.d + kTile - 1) / kTile;
-    return (a.splits * n_rb + n_vt) * dt;
+__device__ __forceinline__ Plan make_plan(const GemmArgs &a, int n_live, int n_clusters) {
+    Plan p;
+    p.n_live = n_live;
+    p.n_rb = (n_live + kTile - 1) / kTile;
+    p.dt = (a.d + kTile - 1) / kTile;
+    p.n_vt = MODE == kModeGrads ? (a.kp + kTile - 1) / kTile : logit_blocks(a.kp, p.n_rb, n_clusters);
+    p.n_blocks = MODE == kModeGrads ? (a.splits * p.n_rb + p.n_vt) * p.dt : p.n_rb * p.n_vt;
+    return p;
 }
 
 template <int MODE>
-__device__ __forceinline__ Block block_at(const GemmArgs &a, int i, int n_live, int n_rb) {
+__device__ __forceinline__ Block block_at(const GemmArgs &a, const Plan &p, int i) {
     Block b;
     if (MODE != kModeGrads) {
-        b.n = i / n_rb;
-        b.m = i % n_rb;
+        b.n = i / p.n_rb;
+        b.m = i % p.n_rb;
+        cut_columns(b, (a.kp + 63) / 64, p.n_vt);
         b.k0 = 0;
         b.ks = a.d / kBlockK;
         b.slice = 0;
         return b;
     }
-    const int dt = (a.d + kTile - 1) / kTile;
-    const int n_dx = a.splits * n_rb * dt;
+    const int n_dx = a.splits * p.n_rb * p.dt;  // the longer ones first
     if (i < n_dx) {
-        const int per = n_rb * dt;
+        const int per = p.n_rb * p.dt;
         b.slice = i / per;
-        b.m = (i % per) / dt;
-        b.n = i % dt;
+        b.m = (i % per) / p.dt;
+        b.n = i % p.dt;
         const int kb = (a.kp + kBlockK - 1) / kBlockK;
         b.k0 = (int)((long long)kb * b.slice / a.splits);
         b.ks = (int)((long long)kb * (b.slice + 1) / a.splits) - b.k0;
     } else {
         const int j = i - n_dx;
         b.slice = -1;
-        b.m = j / dt;
-        b.n = j % dt;
+        b.m = j / p.dt;
+        b.n = j % p.dt;
         b.k0 = 0;
-        b.ks = (n_live + kBlockK - 1) / kBlockK;
+        b.ks = (p.n_live + kBlockK - 1) / kBlockK;
     }
+    cut_columns(b, a.d / 64, p.dt);
     return b;
 }
+
+// ---- blocks handed out at run time: a cluster takes the next one when its producer starts on the one before, so that none
+// ends long after the others.  A warp of the leader CTA draws the numbers and puts them into a small queue in both CTAs'
+// shared memory, tagged with their place in the sequence; every other role reads the whole sequence and reports each
+// entry read, which frees the entry for the number kQueue places further.
+constexpr int kQueue = 4;
+constexpr int kQueueReaders = 2 * (2 + 4) + 1;  // both CTAs' producers and epilogue warps, the MMA warp
+
+struct QueueReader {
+    const volatile unsigned long long *queue;
+    uint32_t freed;  // the leader's barriers
+    uint32_t seq;
+    volatile int *abort_flag;
+    // the next block's number; -1 at the end, -2 if it did not arrive.  By all lanes of a converged warp.
+    __device__ __forceinline__ int next() {
+        int v = -2;
+        if ((threadIdx.x & 31) == 0) {
+            unsigned long long e = queue[seq % kQueue];
+            if ((uint32_t)(e >> 32) != seq + 1) {
+                const long long t0 = clock64();
+                int spins = 0;
+                while ((uint32_t)((e = queue[seq % kQueue]) >> 32) != seq + 1)
+                    if ((++spins & 63) == 0 && (*abort_flag || clock64() - t0 > kWaitLimitCycles)) break;
+            }
+            if ((uint32_t)(e >> 32) == seq + 1) {
+                v = (int)(uint32_t)e;
+                mbar_arrive_cluster(freed + 8 * (seq % kQueue));
+            }
+        }
+        ++seq;
+        return __shfl_sync(0xffffffffu, v, 0);
+    }
+};
 
 // Descriptor of an MN-major bf16 tile in the 128-byte swizzle: 64 elements of the outer axis are one 128-byte row, 8 steps
 // of the reduction axis one 1024-byte group, and the next 64 elements lie 64 reduction steps further.
@@ -195,30 +258,35 @@ struct PatchWriter {
     }
 };
 
-// One CTA per SM, persistent, blocks handed out in turn.  Warp 0: TMA of the A operand; warp 2: of B; warp 1: TMEM and, in
-// the leader CTA, the MMAs; warps 4-7: epilogue.  Every wait is bounded; a role that gives up records an error word and the
-// CTA leaves through the common exit.
+// One CTA per SM, persistent.  Warp 0: TMA of the A operand; warp 2: of B; warp 1: TMEM and, in the leader CTA, the MMAs;
+// warp 3 of the leader CTA: the queue of blocks; warps 4-7: epilogue.  Every wait is bounded; a role that gives up records an
+// error word and the CTA leaves through the common exit.
 template <int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant__ CUtensorMap map_gw, const GemmArgs a) {
     pdl_launch_dependents();
     extern __shared__ __align__(1024) unsigned char vocab_smem[];
-    __shared__ __align__(8) unsigned long long bars[2 * kStages + 4];
+    __shared__ __align__(8) unsigned long long bars[2 * kStages + 4 + kQueue];
+    __shared__ __align__(8) unsigned long long s_queue[kQueue];
     __shared__ uint32_t s_tmem_base;
-    __shared__ int s_abort;
+    __shared__ int s_abort, s_prod_seq;
     const uint32_t ring = (smem_u32(vocab_smem) + 1023u) & ~1023u;
     const uint32_t patches = ring + kStages * kStageBytes;
     const uint32_t bar_full = smem_u32(&bars[0]);                 // used in the leader CTA only
     const uint32_t bar_empty = smem_u32(&bars[kStages]);          // one set per CTA
     const uint32_t bar_tfull = smem_u32(&bars[2 * kStages]);      // one set per CTA
     const uint32_t bar_tempty = smem_u32(&bars[2 * kStages + 2]); // used in the leader CTA only
+    const uint32_t bar_qfree = smem_u32(&bars[2 * kStages + 4]);  // used in the leader CTA only
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const bool leader = rank == 0;
+    if (threadIdx.x < kQueue) s_queue[threadIdx.x] = 0ull;
     if (threadIdx.x == 0) {
         s_abort = 0;
+        s_prod_seq = -1;
         for (int i = 0; i < kStages; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(bar_tfull + 8 * i, 1); mbar_init(bar_tempty + 8 * i, 8); }
+        for (int i = 0; i < kQueue; ++i) mbar_init(bar_qfree + 8 * i, kQueueReaders);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -230,11 +298,9 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
     const uint32_t tmem_base = s_tmem_base;
     volatile int *abort_flag = &s_abort;
     pdl_wait();
-    const int n_live = __ldcg(a.meta_live);
-    const int n_rb = (n_live + kTile - 1) / kTile;
-    const int n_blocks = block_count<MODE>(a, n_rb);
-    const int cluster = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
+    const Plan plan = make_plan<MODE>(a, __ldcg(a.meta + kLive), (int)gridDim.x >> 1);
     const uint32_t full0 = mapa(bar_full, 0), tempty0 = mapa(bar_tempty, 0);
+    QueueReader queue = {s_queue, mapa(bar_qfree, 0), 0, abort_flag};
     bool ok = true;
     int code = 0;
 
@@ -243,8 +309,15 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
         const bool is_a = warp == 0;
         asm volatile("fence.proxy.async;" ::: "memory");  // what the kernels in front wrote is read through the async proxy
         uint32_t s = 0, ph = 0;
-        for (int i = cluster; i < n_blocks && ok; i += n_clusters) {
-            const Block b = block_at<MODE>(a, i, n_live, n_rb);
+        while (ok) {
+            const int i = queue.next();
+            if (i < 0) { ok = i == -1; break; }
+            if (is_a && lane == 0) *reinterpret_cast<volatile int *>(&s_prod_seq) = (int)queue.seq - 1;
+            const Block b = block_at<MODE>(a, plan, i);
+            const int half = b.cols / 2;                   // columns whose operand rows this CTA loads
+            const int b0 = b.c0 + half * (int)rank;
+            // the reduction axis innermost: 32 rows a time at least; outermost: boxes of 64 columns
+            const uint32_t bytes = 2 * (kOperandBytes + (MODE != kModeGrads ? half * kBlockK * 2 : (half + 63) / 64 * (64 * kBlockK * 2)));
             for (int k = b.k0; k < b.k0 + b.ks; ++k) {
                 ok = __all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * s, ph ^ 1u, abort_flag));
                 if (!ok) break;
@@ -252,14 +325,23 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                 const uint32_t full = full0 + 8 * s;
                 if (elect_one()) {
                     if (is_a) {
-                        if (leader) mbar_expect_tx(bar_full + 8 * s, 2 * kStageBytes);  // both operands, both CTAs
+                        if (leader) mbar_expect_tx(bar_full + 8 * s, bytes);  // both operands, both CTAs
                         if (MODE != kModeGrads) tma_load_2d_pair(dst, &maps.x_k, k * kBlockK, b.m * kTile + 128 * (int)rank, full);
                         else if (b.slice >= 0) tma_load_2d_pair(dst, &maps.g_k, k * kBlockK, b.m * kTile + 128 * (int)rank, full);
                         else tma_load_3d_pair(dst, &maps.g_mn, 0, k * kBlockK, 4 * b.m + 2 * (int)rank, full);
+                    } else if (MODE != kModeGrads) {
+                        int r = 0;
+#pragma unroll
+                        for (int lvl = 0; lvl < 3; ++lvl)
+                            if (half - r >= 128 >> lvl) {
+                                tma_load_2d_pair(dst + r * 128, &maps.w_k[lvl], k * kBlockK, a.v0 + b0 + r, full);
+                                r += 128 >> lvl;
+                            }
                     } else {
-                        if (MODE != kModeGrads) tma_load_2d_pair(dst, &maps.w_k, k * kBlockK, a.v0 + b.n * kTile + 128 * (int)rank, full);
-                        else if (b.slice >= 0) tma_load_3d_pair(dst, &maps.w_mn, 0, a.v0 + k * kBlockK, 4 * b.n + 2 * (int)rank, full);
-                        else tma_load_3d_pair(dst, &maps.x_mn, 0, k * kBlockK, 4 * b.n + 2 * (int)rank, full);
+                        const CUtensorMap *m = b.slice >= 0 ? &maps.w_mn : &maps.x_mn;
+                        const int k_at = (b.slice >= 0 ? a.v0 : 0) + k * kBlockK;
+                        tma_load_2d_pair(dst, m, b0, k_at, full);
+                        if (half > 64) tma_load_2d_pair(dst + 64 * kBlockK * 2, m, b0 + 64, k_at, full);
                     }
                 }
                 __syncwarp();
@@ -271,11 +353,13 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
         // ------------------------------------------------------------------ MMA issuer (leader CTA)
         if (leader) {
             uint32_t s = 0, ph = 0, count = 0;
-            for (int i = cluster; i < n_blocks && ok; i += n_clusters) {
-                const Block b = block_at<MODE>(a, i, n_live, n_rb);
+            while (ok) {
+                const int i = queue.next();
+                if (i < 0) { ok = i == -1; break; }
+                const Block b = block_at<MODE>(a, plan, i);
                 if (MODE == kModeGrads && b.slice >= 0 && b.ks == 0) continue;  // an empty slice of a short piece adds nothing
                 const bool a_mn = MODE == kModeGrads && b.slice < 0, b_mn = MODE == kModeGrads;
-                const uint32_t idesc = instr_desc_pair(kTile) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
+                const uint32_t idesc = instr_desc_pair(b.cols) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
                 const uint64_t a0 = a_mn ? smem_desc_sw128_mn(ring) : smem_desc_sw128(ring);
                 const uint64_t b0 = b_mn ? smem_desc_sw128_mn(ring + kOperandBytes) : smem_desc_sw128(ring + kOperandBytes);
                 // a 16-element slice of the reduction axis: 32 bytes further in the swizzle row, or two 8-step groups
@@ -306,21 +390,54 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
             }
             code = 32;
         }
-    } else if (warp >= 4) {
+    } else if (warp == 3) {
+        // ------------------------------------------------------------------ the queue of blocks (leader CTA)
+        if (leader) {
+            const uint32_t peer = mapa(smem_u32(s_queue), 1);
+            const volatile int *prod_seq = &s_prod_seq;
+            for (uint32_t seq = 0; ok; ++seq) {
+                ok = __all_sync(0xffffffffu, mbar_wait(bar_qfree + 8 * (seq % kQueue), ((seq / kQueue) & 1u) ^ 1u, abort_flag));
+                if (!ok) break;
+                int i = -1;
+                if (lane == 0) {
+                    const long long t0 = clock64();
+                    int spins = 0;
+                    while ((int)seq > *prod_seq + 1) {  // (the place behind the block that the producer is on)
+                        __nanosleep(32);
+                        if ((++spins & 63) == 0 && (*abort_flag || clock64() - t0 > kWaitLimitCycles)) { ok = false; break; }
+                    }
+                    if (ok) {
+                        const int ticket = atomicAdd(a.meta + kNextBlock, 1);
+                        // every cluster draws one number behind the last block: the last of them sets the counter back
+                        if (ticket == plan.n_blocks + ((int)gridDim.x >> 1) - 1) atomicExch(a.meta + kNextBlock, 0);
+                        if (ticket < plan.n_blocks) i = ticket;
+                        const unsigned long long e = ((unsigned long long)(seq + 1) << 32) | (uint32_t)i;
+                        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(peer + 8 * (seq % kQueue)), "l"(e) : "memory");
+                        *reinterpret_cast<volatile unsigned long long *>(&s_queue[seq % kQueue]) = e;
+                    }
+                }
+                ok = __shfl_sync(0xffffffffu, ok, 0);
+                if (!ok || __shfl_sync(0xffffffffu, i, 0) < 0) break;
+            }
+            code = 34;
+        }
+    } else {
         // ------------------------------------------------------------------ epilogue
         const int q = warp & 3;
         PatchWriter out = {patches + (uint32_t)q * 2 * kStoreBytes, lane, 0};
         uint32_t count = 0;
-        for (int i = cluster; i < n_blocks && ok; i += n_clusters) {
-            const Block b = block_at<MODE>(a, i, n_live, n_rb);
+        while (ok) {
+            const int i = queue.next();
+            if (i < 0) { ok = i == -1; break; }
+            const Block b = block_at<MODE>(a, plan, i);
             if (MODE == kModeGrads && b.slice >= 0 && b.ks == 0) continue;
             const uint32_t buf = count & 1u, tph = (count >> 1) & 1u;
             ++count;
             const int row = b.m * kTile + 128 * (int)rank + 32 * q + lane;  // of the block's rows, this thread's
-            const int v_first = a.v0 + b.n * kTile;                         // logits: vocabulary row of column 0
+            const int v_first = a.v0 + b.c0;                                // logits: vocabulary row of column 0
             int label = -1;
             float lse2 = 0.f, g = 0.f, gl = 0.f;
-            if (MODE != kModeGrads && row < n_live) {
+            if (MODE != kModeGrads && row < plan.n_live) {
                 label = __ldcg(a.row_target + row) - v_first;  // column of the target, if it is one of the block's
                 if (MODE == kModeDl) {
                     lse2 = __ldcg(a.row_lse2 + row);
@@ -339,12 +456,12 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
             };
             if (MODE == kModeNll) {
                 float m2 = -INFINITY, sum = 0.f;  // of the logits in units of ln 2, without the target's
-                for (int c0 = 0; c0 < kTile; c0 += 32) {
+                for (int c0 = 0; c0 < b.cols; c0 += 32) {
                     float v[32];
                     tmem_ld32(t0 + c0, v);
-                    if (c0 + 32 == kTile) release();
+                    if (c0 + 32 == b.cols) release();
                     const unsigned hit = (unsigned)(label - c0);
-                    if (__any_sync(0xffffffffu, hit < 32u)) {
+                    if (__any_sync(0xffffffffu, hit < 32u && label < b.cols)) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
                             if (hit == (unsigned)j) {
@@ -368,16 +485,16 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                     sum = (s4[0] + s4[1]) + (s4[2] + s4[3]);
                     m2 = m_new;
                 }
-                if (row < n_live) a.part[(size_t)b.n * a.part_ld + row] = make_float2(m2, sum);
+                if (row < plan.n_live) a.part[(size_t)row * a.part_ld + b.n] = make_float2(m2, sum);
             } else if (MODE == kModeDl) {
-                const bool live = row < n_live;
-                for (int c0 = 0; c0 < kTile; c0 += 64) {
+                const bool live = row < plan.n_live;
+                for (int c0 = 0; c0 < b.cols; c0 += 64) {
                     const uint32_t patch = out.begin();
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         float v[32];
                         tmem_ld32(t0 + c0 + 32 * half, v);
-                        if (c0 + 64 == kTile && half == 1) release();
+                        if (c0 + 64 == b.cols && half == 1) release();
                         const int c = c0 + 32 * half;
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = live ? g * exp2_fast(fmaf(v[j], kLog2e, -lse2)) : 0.f;
@@ -397,34 +514,33 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                             out.put(patch, 4 * half + p, make_uint4(pack_bf16(v[8 * p], v[8 * p + 1]), pack_bf16(v[8 * p + 2], v[8 * p + 3]),
                                                                     pack_bf16(v[8 * p + 4], v[8 * p + 5]), pack_bf16(v[8 * p + 6], v[8 * p + 7])));
                     }
-                    out.end([&]() { tma_store_2d(&maps.g_store, b.n * kTile + c0, b.m * kTile + 128 * (int)rank + 32 * q, patch); });
+                    out.end([&]() { tma_store_2d(&maps.g_store, b.c0 + c0, b.m * kTile + 128 * (int)rank + 32 * q, patch); });
                 }
             } else if (b.slice >= 0) {
                 const int row0 = b.slice * a.dx_pitch + b.m * kTile + 128 * (int)rank + 32 * q;
-                for (int c0 = 0; c0 < kTile; c0 += 32) {
-                    if (b.n * kTile + c0 >= a.d) break;
+                for (int c0 = 0; c0 < b.cols; c0 += 32) {
                     const uint32_t patch = out.begin();
                     float v[32];
                     tmem_ld32(t0 + c0, v);
+                    if (c0 + 32 == b.cols) release();
 #pragma unroll
                     for (int p = 0; p < 8; ++p)
                         out.put(patch, p, make_uint4(__float_as_uint(v[4 * p]), __float_as_uint(v[4 * p + 1]), __float_as_uint(v[4 * p + 2]),
                                                      __float_as_uint(v[4 * p + 3])));
                     out.end([&]() {
-                        if (a.first) tma_store_2d(&maps.dx_store, b.n * kTile + c0, row0, patch);
-                        else tma_add_2d(&maps.dx_store, b.n * kTile + c0, row0, patch);
+                        if (a.first) tma_store_2d(&maps.dx_store, b.c0 + c0, row0, patch);
+                        else tma_add_2d(&maps.dx_store, b.c0 + c0, row0, patch);
                     });
                 }
-                release();
             } else {
                 const int v_row0 = a.v0 + b.m * kTile + 128 * (int)rank + 32 * q;
-                for (int c0 = 0; c0 < kTile; c0 += 64) {
-                    if (b.n * kTile + c0 >= a.d || v_row0 >= a.V) break;
+                for (int c0 = 0; c0 < b.cols; c0 += 64) {
                     const uint32_t patch = out.begin();
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         float v[32];
                         tmem_ld32(t0 + c0 + 32 * half, v);
+                        if (c0 + 64 == b.cols && half == 1) release();
                         if (b.ks == 0) {  // no token carries loss: nothing was accumulated
 #pragma unroll
                             for (int j = 0; j < 32; ++j) v[j] = 0.f;
@@ -434,9 +550,10 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                             out.put(patch, 4 * half + p, make_uint4(pack_bf16(v[8 * p], v[8 * p + 1]), pack_bf16(v[8 * p + 2], v[8 * p + 3]),
                                                                     pack_bf16(v[8 * p + 4], v[8 * p + 5]), pack_bf16(v[8 * p + 6], v[8 * p + 7])));
                     }
-                    out.end([&]() { tma_store_2d(&map_gw, b.n * kTile + c0, v_row0, patch); });
+                    out.end([&]() {
+                        if (v_row0 < a.V) tma_store_2d(&map_gw, b.c0 + c0, v_row0, patch);
+                    });
                 }
-                release();
             }
         }
         if (lane == 0) bulk_wait_all();
@@ -460,7 +577,7 @@ struct RowArgs {
     const int32_t *target;
     int T, V, d;
     __nv_bfloat16 *xc;
-    int32_t *meta_live, *row_token, *row_target;
+    int32_t *meta, *row_token, *row_target;
     float *nll, *lse;                              // forward: zeros for tokens without a target
     const float *nll_in, *lse_in, *grad_in;        // backward
     float *row_lse2, *row_g, *row_gl;
@@ -468,50 +585,75 @@ struct RowArgs {
 };
 
 // Rows that carry loss to the front, in their order: each CTA counts the targets in front of its share of the tokens (all
-// of them once, from L2) and copies its rows.  For the gradients the last row block is filled up with zeros: its rows are
-// reduction steps of grad_w.
+// of them once, from L2) and copies its rows, a warp a token.  For the gradients the last row block is filled up with
+// zeros: its rows are reduction steps of grad_w.  Latency is what it costs: a warp's first row is fetched before its place
+// is known, and the targets many at a time.
+constexpr int kRowChunks = 8;    // 16-byte pieces of a row that a lane fetches at a time
+constexpr int kRowTargets = 16;  // targets that a thread fetches at a time
 template <bool BACKWARD>
 __global__ void __launch_bounds__(kRowThreads)
 vocab_rows_kernel(const RowArgs a, int token_ctas) {
     pdl_launch_dependents();
-    __shared__ int s_sum[2][kRowThreads / 32];
+    __shared__ int s_sum[3][kRowThreads / 32];
     __shared__ int s_row[kRowThreads];
-    pdl_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    constexpr int kWarps = kRowThreads / 32;
     const int share = (a.T + token_ctas - 1) / token_ctas;
-    const int t0 = min(blockIdx.x * share, a.T), t1 = min(t0 + share, a.T);
-    auto live_at = [&](int t) { return (unsigned)__ldcg(a.target + t) < (unsigned)a.V; };
+    const int t0 = (int)min((long long)blockIdx.x * share, (long long)a.T), t1 = min(t0 + share, a.T);
+    const int chunks = a.d / 8;
+    pdl_wait();
+    if (blockIdx.x == 0 && tid == 0) a.meta[kNextBlock] = 0;
+    auto fetch = [&](int t, int c0, uint4 (&v)[kRowChunks]) {
+        const uint4 *src = reinterpret_cast<const uint4 *>(a.x + (size_t)t * a.d);
+#pragma unroll
+        for (int i = 0; i < kRowChunks; ++i)
+            if (c0 + 32 * i + lane < chunks) v[i] = __ldcg(src + c0 + 32 * i + lane);
+    };
+    auto live = [&](int target) { return (unsigned)target < (unsigned)a.V; };
+    uint4 v[kRowChunks];
+    int target = t0 + tid < t1 ? __ldcg(a.target + t0 + tid) : -1;
+    if (t0 + warp < t1) fetch(t0 + warp, 0, v);
     int before = 0, total = 0;
-#pragma unroll 8
-    for (int t = tid; t < a.T; t += kRowThreads) {
-        const int l = live_at(t) ? 1 : 0;
-        total += l;
-        before += t < t0 ? l : 0;
+    for (int base = tid; base < a.T; base += kRowThreads * kRowTargets) {
+        float f[kRowTargets];
+#pragma unroll
+        for (int i = 0; i < kRowTargets; ++i) {
+            const int t = base + i * kRowThreads;
+            f[i] = ldcg_if(t < a.T, reinterpret_cast<const float *>(a.target) + t, __int_as_float(-1));
+        }
+#pragma unroll
+        for (int i = 0; i < kRowTargets; ++i) {
+            const int l = live(__float_as_int(f[i])) ? 1 : 0;
+            total += l;
+            before += base + i * kRowThreads < t0 ? l : 0;
+        }
     }
     before = __reduce_add_sync(0xffffffffu, before);
     total = __reduce_add_sync(0xffffffffu, total);
     if (lane == 0) { s_sum[0][warp] = before; s_sum[1][warp] = total; }
-    __syncthreads();
     before = total = 0;
-    for (int w = 0; w < kRowThreads / 32; ++w) { before += s_sum[0][w]; total += s_sum[1][w]; }
-    if (blockIdx.x == 0 && tid == 0) *a.meta_live = total;
-    const int chunks = a.d / 8;
-    for (int sub = t0; sub < t1; sub += kRowThreads) {
-        __syncthreads();
+    for (int sub = t0; sub == t0 || sub < t1; sub += kRowThreads) {
         const int t = sub + tid;
-        const bool live = t < t1 && live_at(t);
-        const unsigned vote = __ballot_sync(0xffffffffu, live);
-        if (lane == 0) s_sum[0][warp] = __popc(vote);
-        __syncthreads();
-        int row = before + __popc(vote & ((1u << lane) - 1u));
-        for (int w = 0; w < kRowThreads / 32; ++w) {
-            if (w < warp) row += s_sum[0][w];
-            before += s_sum[0][w];
+        if (sub > t0) {
+            __syncthreads();
+            target = t < t1 ? __ldcg(a.target + t) : -1;
         }
+        const bool on = live(target);
+        const unsigned vote = __ballot_sync(0xffffffffu, on);
+        if (lane == 0) s_sum[2][warp] = __popc(vote);
+        __syncthreads();
+        if (sub == t0)
+            for (int w = 0; w < kWarps; ++w) { before += s_sum[0][w]; total += s_sum[1][w]; }
+        int row = before + __popc(vote & ((1u << lane) - 1u));
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) row += s_sum[2][w];
+            before += s_sum[2][w];
+        }
+        s_row[tid] = on ? row : -1;
         if (t < t1) {
-            if (live) {
+            if (on) {
                 a.row_token[row] = t;
-                a.row_target[row] = __ldcg(a.target + t);
+                a.row_target[row] = target;
                 if (BACKWARD) {
                     const float g = __ldcg(a.grad_in + t);
                     a.row_lse2[row] = __ldcg(a.lse_in + t) * kLog2e;
@@ -523,87 +665,107 @@ vocab_rows_kernel(const RowArgs a, int token_ctas) {
                 a.lse[t] = 0.f;
             }
         }
-        s_row[tid] = live ? row : -1;
         __syncthreads();
-        for (int i = warp; i < min(kRowThreads, t1 - sub); i += kRowThreads / 32) {
+        for (int i = warp; i < min(kRowThreads, t1 - sub); i += kWarps) {
             const int r = s_row[i];
-            if (r >= 0) {
-                const uint4 *src = reinterpret_cast<const uint4 *>(a.x + (size_t)(sub + i) * a.d);
-                uint4 *dst = reinterpret_cast<uint4 *>(a.xc + (size_t)r * a.d);
-#pragma unroll 4
-                for (int c = lane; c < chunks; c += 32) dst[c] = __ldcg(src + c);
-            } else if (BACKWARD) {
-                uint4 *dst = reinterpret_cast<uint4 *>(a.grad_x + (size_t)(sub + i) * a.d);
-                for (int c = lane; c < chunks; c += 32) dst[c] = make_uint4(0, 0, 0, 0);
+            uint4 *dst = reinterpret_cast<uint4 *>(r >= 0 ? a.xc + (size_t)r * a.d : a.grad_x + (size_t)(sub + i) * a.d);
+            for (int c0 = 0; c0 < chunks; c0 += 32 * kRowChunks) {
+                if (r < 0) {
+                    if (!BACKWARD) break;
+#pragma unroll
+                    for (int k = 0; k < kRowChunks; ++k) v[k] = make_uint4(0, 0, 0, 0);
+                } else if (sub > t0 || i != warp || c0 > 0) {
+                    fetch(sub + i, c0, v);
+                }
+#pragma unroll
+                for (int k = 0; k < kRowChunks; ++k)
+                    if (c0 + 32 * k + lane < chunks) dst[c0 + 32 * k + lane] = v[k];
             }
         }
     }
+    if (blockIdx.x == 0 && tid == 0) a.meta[kLive] = total;
     if (BACKWARD) {
         const int end = (total + kTile - 1) / kTile * kTile;
-        for (int r = total + blockIdx.x * (kRowThreads / 32) + warp; r < end; r += gridDim.x * (kRowThreads / 32)) {
+        for (int r = total + blockIdx.x * kWarps + warp; r < end; r += gridDim.x * kWarps) {
             uint4 *dst = reinterpret_cast<uint4 *>(a.xc + (size_t)r * a.d);
             for (int c = lane; c < chunks; c += 32) dst[c] = make_uint4(0, 0, 0, 0);
         }
     }
 }
 
-// The partial maxima and sums of a token's logits, and its likelihood.  A warp takes every sixteenth block of 256 logits
-// of 32 rows (a lane each).  The target's logit was kept apart: nll = log(1 + sum of the others' exp(l - l_target)) keeps
-// its digits where the target is nearly certain.
-constexpr int kNllWarps = 16;
+// The partial maxima and sums of a token's logits, and its likelihood: a warp a row.  The target's logit was kept apart:
+// nll = log(1 + sum of the others' exp(l - l_target)) keeps its digits where the target is nearly certain.
+constexpr int kNllWarps = 8;
+constexpr int kNllBatch = 16;  // partial results that a lane fetches at a time
 __global__ void __launch_bounds__(32 * kNllWarps)
-vocab_nll_kernel(const int32_t *__restrict__ meta_live, const float2 *__restrict__ part, int part_ld, int n_vt,
+vocab_nll_kernel(const int32_t *__restrict__ meta, const float2 *__restrict__ part, int part_ld, int V, int n_clusters,
                  const int32_t *__restrict__ row_token, const float *__restrict__ row_label, float *__restrict__ nll,
                  float *__restrict__ lse) {
     pdl_launch_dependents();
-    __shared__ float2 sh[kNllWarps][32];
     pdl_wait();
-    const int n_live = __ldcg(meta_live);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int row = blockIdx.x * 32 + lane;
-    auto join = [](float2 &acc, float2 p) {
-        const float m = fmaxf(acc.x, p.x), ref = m == -INFINITY ? 0.f : m;
-        acc = make_float2(m, acc.y * exp2_fast(acc.x - ref) + p.y * exp2_fast(p.x - ref));
-    };
-    float2 acc = make_float2(-INFINITY, 0.f);
-    if (row < n_live) {
-#pragma unroll 8
-        for (int b = warp; b < n_vt; b += kNllWarps) join(acc, __ldcg(part + (size_t)b * part_ld + row));
-    }
-    sh[warp][lane] = acc;
-    __syncthreads();
-    if (warp != 0 || row >= n_live) return;
-    for (int w = 1; w < kNllWarps; ++w) join(acc, sh[w][lane]);
+    const int n_live = __ldcg(meta + kLive);
+    const int lane = threadIdx.x & 31;
+    const int row = blockIdx.x * kNllWarps + (threadIdx.x >> 5);
+    if (row >= n_live) return;
+    const int n_vt = logit_blocks(V, (n_live + kTile - 1) / kTile, n_clusters);
+    const float2 *src = part + (size_t)row * part_ld;
     const float at = __ldcg(row_label + row);
-    const float ahead = fmaf(at, -kLog2e, acc.x);  // of the others' largest logit, in units of ln 2
-    const float loss = ahead > 0.f ? (ahead + log2f(acc.y + exp2f(-ahead))) * kLn2 : log1pf(acc.y * exp2f(ahead));
     const int t = __ldcg(row_token + row);
+    float m = -INFINITY, sum = 0.f;
+    for (int b0 = lane; b0 < n_vt; b0 += 32 * kNllBatch) {
+        float pm[kNllBatch], ps[kNllBatch];
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < kNllBatch; ++i) {
+            const int b = b0 + 32 * i;
+            pm[i] = ldcg_if(b < n_vt, reinterpret_cast<const float *>(src + b), -INFINITY);
+            ps[i] = ldcg_if(b < n_vt, reinterpret_cast<const float *>(src + b) + 1, 0.f);
+        }
+#pragma unroll
+        for (int i = 0; i < kNllBatch; ++i) top = fmaxf(top, pm[i]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        sum *= exp2_fast(m - ref);
+#pragma unroll
+        for (int i = 0; i < kNllBatch; ++i) sum = fmaf(ps[i], exp2_fast(pm[i] - ref), sum);
+        m = top;
+    }
+    float top = m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    sum *= exp2_fast(m - (top == -INFINITY ? 0.f : top));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane != 0) return;
+    const float ahead = fmaf(at, -kLog2e, top);  // of the others' largest logit, in units of ln 2
+    const float loss = ahead > 0.f ? (ahead + log2f(sum + exp2f(-ahead))) * kLn2 : log1pf(sum * exp2f(ahead));
     nll[t] = loss;
     lse[t] = at + loss;
 }
 
-// grad_x: the slices' sums of a row, rounded, to its token
+// grad_x: the slices' sums of a row, rounded, to its token; a warp takes 256 columns
 __global__ void __launch_bounds__(kRowThreads)
-vocab_grad_x_kernel(const int32_t *__restrict__ meta_live, const float *__restrict__ dx, int splits, size_t slice_stride, int d,
+vocab_grad_x_kernel(const int32_t *__restrict__ meta, const float *__restrict__ dx, int splits, size_t slice_stride, int d,
                     const int32_t *__restrict__ row_token, __nv_bfloat16 *__restrict__ grad_x) {
     pdl_launch_dependents();
     pdl_wait();
-    const int n_live = __ldcg(meta_live);
-    const int lane = threadIdx.x & 31;
-    for (int r = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5); r < n_live; r += gridDim.x * (kRowThreads / 32)) {
+    const int n_live = __ldcg(meta + kLive);
+    const int lane = threadIdx.x & 31, parts = (d + 255) / 256;
+    const long long n = (long long)n_live * parts;
+    for (long long i = (long long)blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5); i < n; i += (long long)gridDim.x * (kRowThreads / 32)) {
+        const int r = (int)(i / parts), c = (int)(i % parts) * 256 + 8 * lane;
+        if (c >= d) continue;
         const int t = __ldcg(row_token + r);
-        const float *src = dx + (size_t)r * d;
-        for (int c = lane; c < d / 8; c += 32) {
-            float4 lo = __ldcg(reinterpret_cast<const float4 *>(src) + 2 * c), hi = __ldcg(reinterpret_cast<const float4 *>(src) + 2 * c + 1);
-            for (int s = 1; s < splits; ++s) {
-                const float4 *p = reinterpret_cast<const float4 *>(src + s * slice_stride) + 2 * c;
-                const float4 l = __ldcg(p), h = __ldcg(p + 1);
-                lo.x += l.x; lo.y += l.y; lo.z += l.z; lo.w += l.w;
-                hi.x += h.x; hi.y += h.y; hi.z += h.z; hi.w += h.w;
-            }
-            *(reinterpret_cast<uint4 *>(grad_x + (size_t)t * d) + c) =
-                make_uint4(pack_bf16(lo.x, lo.y), pack_bf16(lo.z, lo.w), pack_bf16(hi.x, hi.y), pack_bf16(hi.z, hi.w));
+        const float *src = dx + (size_t)r * d + c;
+        float4 lo = __ldcg(reinterpret_cast<const float4 *>(src)), hi = __ldcg(reinterpret_cast<const float4 *>(src) + 1);
+#pragma unroll 4
+        for (int s = 1; s < splits; ++s) {
+            const float4 *p = reinterpret_cast<const float4 *>(src + s * slice_stride);
+            const float4 l = __ldcg(p), h = __ldcg(p + 1);
+            lo.x += l.x; lo.y += l.y; lo.z += l.z; lo.w += l.w;
+            hi.x += h.x; hi.y += h.y; hi.z += h.z; hi.w += h.w;
         }
+        *reinterpret_cast<uint4 *>(grad_x + (size_t)t * d + c) =
+            make_uint4(pack_bf16(lo.x, lo.y), pack_bf16(lo.z, lo.w), pack_bf16(hi.x, hi.y), pack_bf16(hi.z, hi.w));
     }
 }
 
@@ -655,7 +817,8 @@ size_t vocab_carve(const zeda_vocab_config_t &c, unsigned char *base, zeda_vocab
     v.row_token = (int32_t *)take((size_t)v.rows * 4);
     v.row_target = (int32_t *)take((size_t)v.rows * 4);
     v.row_label = (float *)take((size_t)v.rows * 4);
-    v.part = (float2 *)take((size_t)tiles(c.n_vocab) * v.rows * 8);
+    v.part_ld = tiles(c.n_vocab) + kMaxClusters;  // (logit_blocks adds less than a turn)
+    v.part = (float2 *)take((size_t)v.part_ld * v.rows * 8);
     v.xc = (__nv_bfloat16 *)take((size_t)v.rows * c.d_model * 2);
     if (c.backward) {
         v.row_lse2 = (float *)take((size_t)v.rows * 4);
@@ -690,10 +853,11 @@ bool map_mn(CUtensorMap *m, const void *base, size_t steps, size_t cols) {
 
 bool build_maps(zeda_vocab *h, VocabMaps *m) {
     const size_t d = h->cfg.d_model, V = h->cfg.n_vocab;
-    bool ok = map_2d(&m->x_k, h->xc, h->rows, d, kBlockK, 128) && map_2d(&m->w_k, h->w, V, d, kBlockK, 128);
+    bool ok = map_2d(&m->x_k, h->xc, h->rows, d, kBlockK, 128);
+    for (int i = 0; i < 3; ++i) ok = ok && map_2d(&m->w_k[i], h->w, V, d, kBlockK, 128 >> i);
     if (ok && h->cfg.backward) {
-        ok = map_2d(&m->g_k, h->g, h->rows, h->piece, kBlockK, 128) && map_mn(&m->x_mn, h->xc, h->rows, d) && map_mn(&m->w_mn, h->w, V, d) &&
-             map_mn(&m->g_mn, h->g, h->rows, h->piece) && map_2d(&m->g_store, h->g, h->rows, h->piece, 64, 32);
+        ok = map_2d(&m->g_k, h->g, h->rows, h->piece, kBlockK, 128) && map_2d(&m->x_mn, h->xc, h->rows, d, 64, kBlockK) &&
+             map_2d(&m->w_mn, h->w, V, d, 64, kBlockK) && map_mn(&m->g_mn, h->g, h->rows, h->piece) && map_2d(&m->g_store, h->g, h->rows, h->piece, 64, 32);
         const cuuint64_t dims[2] = {d, (cuuint64_t)h->dx_rows}, strides[1] = {d * 4};
         const cuuint32_t box[2] = {32, 32};
         ok = ok && encode_f32_map(&m->dx_store, h->dx, 2, dims, strides, box);
@@ -701,21 +865,23 @@ bool build_maps(zeda_vocab *h, VocabMaps *m) {
     return ok;
 }
 
+int clusters(const zeda_vocab *h) { return h->sm_count / 2 < kMaxClusters ? h->sm_count / 2 : kMaxClusters; }
+
 template <int MODE>
 cudaError_t launch_gemm(const zeda_vocab *h, const CUtensorMap &map_gw, const GemmArgs &a, cudaStream_t s) {
-    return launch_kernel(h->pdl, vocab_gemm_kernel<MODE>, dim3(h->sm_count / 2 * 2), dim3(kGemmThreads), (size_t)kGemmSmem, s,
+    return launch_kernel(h->pdl, vocab_gemm_kernel<MODE>, dim3(2 * clusters(h)), dim3(kGemmThreads), (size_t)kGemmSmem, s,
                          *static_cast<const VocabMaps *>(h->maps), map_gw, a);
 }
 
 template <bool BACKWARD>
 cudaError_t launch_rows(const zeda_vocab *h, RowArgs &a, cudaStream_t s) {
-    int token_ctas = (a.T + 15) / 16;
-    if (token_ctas > 2 * h->sm_count) token_ctas = 2 * h->sm_count;
+    int token_ctas = (a.T + kRowThreads / 32 - 1) / (kRowThreads / 32);  // a token a warp, up to a limit
+    if (token_ctas > 4 * h->sm_count) token_ctas = 4 * h->sm_count;
     const int ctas = BACKWARD && token_ctas < 32 ? 32 : token_ctas;  // the others help with the zeros behind the last row
     a.V = h->cfg.n_vocab;
     a.d = h->cfg.d_model;
     a.xc = h->xc;
-    a.meta_live = h->meta + kLive;
+    a.meta = h->meta;
     a.row_token = h->row_token;
     a.row_target = h->row_target;
     a.row_lse2 = h->row_lse2;
@@ -729,7 +895,6 @@ GemmArgs gemm_args(const zeda_vocab *h) {
     a.d = h->cfg.d_model;
     a.V = h->cfg.n_vocab;
     a.kp = h->cfg.n_vocab;
-    a.meta_live = h->meta + kLive;
     a.meta = h->meta;
     a.row_target = h->row_target;
     a.row_label = h->row_label;
@@ -737,7 +902,7 @@ GemmArgs gemm_args(const zeda_vocab *h) {
     a.row_g = h->row_g;
     a.row_gl = h->row_gl;
     a.part = h->part;
-    a.part_ld = h->rows;
+    a.part_ld = h->part_ld;
     return a;
 }
 
@@ -842,8 +1007,9 @@ zeda_status_t zeda_vocab_nll(zeda_vocab_t *h, const void *x, const int32_t *targ
     const GemmArgs a = gemm_args(h);
     const VocabMaps *maps = static_cast<const VocabMaps *>(h->maps);
     if ((e = launch_gemm<kModeNll>(h, maps->x_k, a, s)) != cudaSuccess) return vocab_fail("logits launch", e);
-    e = launch_kernel(h->pdl, vocab_nll_kernel, dim3((T + 31) / 32), dim3(32 * kNllWarps), 0, s, (const int32_t *)(h->meta + kLive),
-                      (const float2 *)h->part, h->rows, tiles(h->cfg.n_vocab), (const int32_t *)h->row_token, (const float *)h->row_label, nll, lse);
+    e = launch_kernel(h->pdl, vocab_nll_kernel, dim3((T + kNllWarps - 1) / kNllWarps), dim3(32 * kNllWarps), 0, s, (const int32_t *)h->meta,
+                      (const float2 *)h->part, h->part_ld, h->cfg.n_vocab, clusters(h), (const int32_t *)h->row_token,
+                      (const float *)h->row_label, nll, lse);
     if (e != cudaSuccess) return vocab_fail("likelihood launch", e);
     return ZEDA_OK;
 }
@@ -903,9 +1069,9 @@ zeda_status_t zeda_vocab_nll_backward(zeda_vocab_t *h, const void *x, const int3
         if ((e = launch_gemm<kModeDl>(h, map_gw, a, s)) != cudaSuccess) return vocab_fail("logits' gradient launch", e);
         if ((e = launch_gemm<kModeGrads>(h, map_gw, a, s)) != cudaSuccess) return vocab_fail("gradients launch", e);
     }
-    int ctas = (T + kRowThreads / 32 - 1) / (kRowThreads / 32);
-    if (ctas > 8 * h->sm_count) ctas = 8 * h->sm_count;
-    e = launch_kernel(h->pdl, vocab_grad_x_kernel, dim3(ctas), dim3(kRowThreads), 0, s, (const int32_t *)(h->meta + kLive),
+    const long long warps = (long long)T * ((a.d + 255) / 256), most = 8 * h->sm_count;
+    int ctas = (int)((warps + kRowThreads / 32 - 1) / (kRowThreads / 32) < most ? (warps + kRowThreads / 32 - 1) / (kRowThreads / 32) : most);
+    e = launch_kernel(h->pdl, vocab_grad_x_kernel, dim3(ctas), dim3(kRowThreads), 0, s, (const int32_t *)h->meta,
                       (const float *)h->dx, a.splits, (size_t)a.dx_pitch * a.d, a.d, (const int32_t *)h->row_token,
                       static_cast<__nv_bfloat16 *>(grad_x));
     if (e != cudaSuccess) return vocab_fail("grad_x launch", e);

@@ -264,9 +264,9 @@ __device__ __forceinline__ uint32_t instr_desc(int n) {
 
 }  // namespace tc
 
-// Host: encode a bf16 tensor map with the 128-byte swizzle (defined in tc_host.cu).
+// Host: encode a bf16 tensor map, with the 128-byte swizzle unless another is named (defined in tc_host.cu).
 bool encode_bf16_map(CUtensorMap *m, const void *base, int rank, const cuuint64_t *dims,
-                     const cuuint64_t *strides_bytes, const cuuint32_t *box);
+                     const cuuint64_t *strides_bytes, const cuuint32_t *box, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B);
 // the same of an fp32 tensor
 bool encode_f32_map(CUtensorMap *m, const void *base, int rank, const cuuint64_t *dims,
                     const cuuint64_t *strides_bytes, const cuuint32_t *box);

@@ -22,12 +22,12 @@ EncodeTiledFn encode_fn() {
 }
 
 bool encode_impl(CUtensorMap *m, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides_bytes,
-                 const cuuint32_t *box, CUtensorMapDataType type) {
+                 const cuuint32_t *box, CUtensorMapDataType type, CUtensorMapSwizzle swizzle) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) { set_error("cuTensorMapEncodeTiled is not available from the driver"); return false; }
     cuuint32_t ones[5] = {1, 1, 1, 1, 1};
     CUresult r = fn(m, type, (cuuint32_t)rank, const_cast<void *>(base), dims, strides_bytes,
-                    box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                    box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) { set_error("cuTensorMapEncodeTiled failed with code %d", (int)r); return false; }
     return true;
@@ -36,13 +36,13 @@ bool encode_impl(CUtensorMap *m, const void *base, int rank, const cuuint64_t *d
 }  // namespace
 
 bool encode_bf16_map(CUtensorMap *m, const void *base, int rank, const cuuint64_t *dims,
-                     const cuuint64_t *strides_bytes, const cuuint32_t *box) {
-    return encode_impl(m, base, rank, dims, strides_bytes, box, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16);
+                     const cuuint64_t *strides_bytes, const cuuint32_t *box, CUtensorMapSwizzle swizzle) {
+    return encode_impl(m, base, rank, dims, strides_bytes, box, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, swizzle);
 }
 
 bool encode_f32_map(CUtensorMap *m, const void *base, int rank, const cuuint64_t *dims,
                     const cuuint64_t *strides_bytes, const cuuint32_t *box) {
-    return encode_impl(m, base, rank, dims, strides_bytes, box, CU_TENSOR_MAP_DATA_TYPE_FLOAT32);
+    return encode_impl(m, base, rank, dims, strides_bytes, box, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 }  // namespace zeda

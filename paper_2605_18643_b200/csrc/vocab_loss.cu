@@ -54,11 +54,17 @@ constexpr int kOperandBytes = 128 * kBlockK * 2; // one CTA's half of an operand
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kStages = 6;
 constexpr int kStoreBytes = 4096;                // an epilogue warp's patch of 32 rows x 128 bytes
-constexpr int kGemmThreads = 256;
+constexpr int kEpilogueWarps = 4, kSwapEpilogueWarps = 8;  // the turned patches cost latency: two warps per quarter of TMEM hide it
+constexpr int gemm_threads(bool swap) { return 128 + 32 * (swap ? kSwapEpilogueWarps : kEpilogueWarps); }
+constexpr int kSwapRing = 5 * kStageBytes;       // the swapped form's patches take a stage's room
+constexpr int kSwapPatches = 16 * kStoreBytes;
 constexpr int kGemmSmem = kStages * kStageBytes + 8 * kStoreBytes + 1024;
+static_assert(kSwapRing + kSwapPatches + 1024 == kGemmSmem, "both forms fill the shared memory");
 constexpr int kRowThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr size_t kPieceBytes = (size_t)256 << 20;  // of dl at a time
+constexpr int kSwapStages = 10;                  // at most, of narrow column blocks
+constexpr int kSwapTokens = 576;                 // calls of at most so many tokens may take them as the columns of the logits
 constexpr int kMaxClusters = 80;                 // CTA pairs of a launch
 constexpr int kMaxSplits = 16;                   // of the vocabulary axis of grad_x
 
@@ -67,11 +73,13 @@ enum VocabMeta { kLive = 0, kVocabError = 1, kNextBlock = 2, kVocabMetaCount = 6
 enum { kModeNll = 0, kModeDl = 1, kModeGrads = 2 };
 
 struct VocabMaps {
-    CUtensorMap x_k, g_k;          // reduction axis innermost: [rows][k], box {64, 128}
-    CUtensorMap w_k[3];            // the same with boxes of 128, 64 and 32 rows: half a block's columns are a multiple of 32
+    // reduction axis innermost: [rows][k], boxes of 64 x 128, 64 and 32 rows (half a block's columns are a multiple of 32, and
+    // of its rows those behind the last token are not loaded)
+    CUtensorMap x_k[3], w_k[3], g_k[3];
     CUtensorMap g_mn;              // reduction axis outermost: (64 elements, k, block of 64), box {64, 64, 2}
     CUtensorMap x_mn, w_mn;        // [k][columns], box {64, 64}
     CUtensorMap g_store;           // [rows][piece], box {64, 32}
+    CUtensorMap g_store_32;        // the same, box {32, 32}, 64-byte swizzle
     CUtensorMap dx_store;          // [dx_rows][d] fp32, box {32, 32}
 };
 
@@ -81,6 +89,7 @@ struct GemmArgs {
     int splits;      // slices of the piece that grad_x is summed in
     int dx_pitch;    // rows between two slices' sums
     int first;       // first piece: the sums start here
+    int back;        // blocks of the logits from the last to the first: the matrix's end is what the pass in front left in L2
     int32_t *meta;
     const int32_t *row_target;
     float *row_label;
@@ -119,9 +128,18 @@ struct Plan {  // of one launch
     int n_live, n_rb, n_vt, dt, n_blocks;
 };
 
-template <int MODE>
+// SWAP (few tokens): the vocabulary gives the blocks' rows and the tokens their columns, which come in units of 64.
+template <int MODE, bool SWAP>
 __device__ __forceinline__ Plan make_plan(const GemmArgs &a, int n_live, int n_clusters) {
     Plan p;
+    if (SWAP) {
+        p.n_live = n_live;
+        p.dt = 0;
+        p.n_vt = (a.kp + kTile - 1) / kTile;
+        p.n_rb = (n_live + kTile - 1) / kTile;  // here: blocks of columns
+        p.n_blocks = p.n_vt * p.n_rb;
+        return p;
+    }
     p.n_live = n_live;
     p.n_rb = (n_live + kTile - 1) / kTile;
     p.dt = (a.d + kTile - 1) / kTile;
@@ -130,9 +148,19 @@ __device__ __forceinline__ Plan make_plan(const GemmArgs &a, int n_live, int n_c
     return p;
 }
 
-template <int MODE>
+template <int MODE, bool SWAP>
 __device__ __forceinline__ Block block_at(const GemmArgs &a, const Plan &p, int i) {
     Block b;
+    if (MODE == kModeDl && a.back) i = p.n_blocks - 1 - i;
+    if (SWAP) {
+        b.m = i / p.n_rb;
+        b.n = i % p.n_rb;
+        cut_columns(b, (p.n_live + 63) / 64, p.n_rb);
+        b.k0 = 0;
+        b.ks = a.d / kBlockK;
+        b.slice = 0;
+        return b;
+    }
     if (MODE != kModeGrads) {
         b.n = i / p.n_rb;
         b.m = i % p.n_rb;
@@ -168,7 +196,6 @@ __device__ __forceinline__ Block block_at(const GemmArgs &a, const Plan &p, int 
 // shared memory, tagged with their place in the sequence; every other role reads the whole sequence and reports each
 // entry read, which frees the entry for the number kQueue places further.
 constexpr int kQueue = 4;
-constexpr int kQueueReaders = 2 * (2 + 4) + 1;  // both CTAs' producers and epilogue warps, the MMA warp
 
 struct QueueReader {
     const volatile unsigned long long *queue;
@@ -232,6 +259,17 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     return *reinterpret_cast<const uint32_t *>(&p);
 }
 
+// n rows (a multiple of 32, at most 128) of an operand whose reduction axis lies innermost, in as few boxes as it takes
+__device__ __forceinline__ void load_rows(const CUtensorMap (&maps)[3], uint32_t dst, int k, int row, int n, uint32_t bar) {
+    int r = 0;
+#pragma unroll
+    for (int lvl = 0; lvl < 3; ++lvl)
+        if (n - r >= 128 >> lvl) {
+            tma_load_2d_pair(dst + r * kBlockK * 2, &maps[lvl], k, row + r, bar);
+            r += 128 >> lvl;
+        }
+}
+
 // One patch of 32 rows x 128 bytes to global memory: lane's row of eight 16-byte pieces into the swizzled layout, then
 // one TMA store (or addition) by one lane.  Two patches per warp: the one before is still being read.
 struct PatchWriter {
@@ -261,22 +299,30 @@ struct PatchWriter {
 // One CTA per SM, persistent.  Warp 0: TMA of the A operand; warp 2: of B; warp 1: TMEM and, in the leader CTA, the MMAs;
 // warp 3 of the leader CTA: the queue of blocks; warps 4-7: epilogue.  Every wait is bounded; a role that gives up records an
 // error word and the CTA leaves through the common exit.
-template <int MODE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
+//
+// SWAP: with few tokens, blocks of 256 token rows would be mostly empty (601 tokens: 768), so W is the M operand and up to
+// 256 tokens, in units of 64, are the N operand.  A thread then reads 32 tokens' logits of one vocabulary row from TMEM; each
+// 32 x 32 patch goes through shared memory, so that from there on a thread again holds a token's logits.
+template <int MODE, bool SWAP>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(gemm_threads(SWAP), 1)
 vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant__ CUtensorMap map_gw, const GemmArgs a) {
     pdl_launch_dependents();
     extern __shared__ __align__(1024) unsigned char vocab_smem[];
-    __shared__ __align__(8) unsigned long long bars[2 * kStages + 4 + kQueue];
+    constexpr int kMaxStages = SWAP ? kSwapStages : kStages;
+    __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 5 + kQueue];
     __shared__ __align__(8) unsigned long long s_queue[kQueue];
     __shared__ uint32_t s_tmem_base;
     __shared__ int s_abort, s_prod_seq;
     const uint32_t ring = (smem_u32(vocab_smem) + 1023u) & ~1023u;
-    const uint32_t patches = ring + kStages * kStageBytes;
-    const uint32_t bar_full = smem_u32(&bars[0]);                 // used in the leader CTA only
-    const uint32_t bar_empty = smem_u32(&bars[kStages]);          // one set per CTA
-    const uint32_t bar_tfull = smem_u32(&bars[2 * kStages]);      // one set per CTA
-    const uint32_t bar_tempty = smem_u32(&bars[2 * kStages + 2]); // used in the leader CTA only
-    const uint32_t bar_qfree = smem_u32(&bars[2 * kStages + 4]);  // used in the leader CTA only
+    constexpr int kEpilogue = SWAP ? kSwapEpilogueWarps : kEpilogueWarps;
+    constexpr uint32_t kRing = SWAP ? kSwapRing : kStages * kStageBytes;
+    const uint32_t patches = ring + kRing;
+    const uint32_t bar_full = smem_u32(&bars[0]);                    // used in the leader CTA only
+    const uint32_t bar_empty = smem_u32(&bars[kMaxStages]);          // one set per CTA
+    const uint32_t bar_tfull = smem_u32(&bars[2 * kMaxStages]);      // one set per CTA
+    const uint32_t bar_tempty = smem_u32(&bars[2 * kMaxStages + 2]); // used in the leader CTA only
+    const uint32_t bar_join = smem_u32(&bars[2 * kMaxStages + 4]);   // SWAP: the epilogue warps' partial results are written
+    const uint32_t bar_qfree = smem_u32(&bars[2 * kMaxStages + 5]);  // used in the leader CTA only
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const bool leader = rank == 0;
@@ -284,9 +330,10 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
     if (threadIdx.x == 0) {
         s_abort = 0;
         s_prod_seq = -1;
-        for (int i = 0; i < kStages; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(bar_tfull + 8 * i, 1); mbar_init(bar_tempty + 8 * i, 8); }
-        for (int i = 0; i < kQueue; ++i) mbar_init(bar_qfree + 8 * i, kQueueReaders);
+        for (int i = 0; i < kMaxStages; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(bar_tfull + 8 * i, 1); mbar_init(bar_tempty + 8 * i, 2 * kEpilogue); }
+        mbar_init(bar_join, kEpilogue);
+        for (int i = 0; i < kQueue; ++i) mbar_init(bar_qfree + 8 * i, 2 * (2 + kEpilogue) + 1);  // the queue's readers: producers, epilogue, MMA warp
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -298,9 +345,13 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
     const uint32_t tmem_base = s_tmem_base;
     volatile int *abort_flag = &s_abort;
     pdl_wait();
-    const Plan plan = make_plan<MODE>(a, __ldcg(a.meta + kLive), (int)gridDim.x >> 1);
+    const Plan plan = make_plan<MODE, SWAP>(a, __ldcg(a.meta + kLive), (int)gridDim.x >> 1);
     const uint32_t full0 = mapa(bar_full, 0), tempty0 = mapa(bar_tempty, 0);
     QueueReader queue = {s_queue, mapa(bar_qfree, 0), 0, abort_flag};
+    // narrow column blocks leave room for more stages of the matrix's rows
+    const int max_half = SWAP ? min(32 * ((plan.n_live + 63) / 64), 128) : 128;
+    const uint32_t stage_bytes = SWAP ? kOperandBytes + max_half * kBlockK * 2 : kStageBytes;
+    const uint32_t stages = SWAP ? min(kRing / stage_bytes, (uint32_t)kMaxStages) : kStages;
     bool ok = true;
     int code = 0;
 
@@ -313,30 +364,30 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
             const int i = queue.next();
             if (i < 0) { ok = i == -1; break; }
             if (is_a && lane == 0) *reinterpret_cast<volatile int *>(&s_prod_seq) = (int)queue.seq - 1;
-            const Block b = block_at<MODE>(a, plan, i);
+            const Block b = block_at<MODE, SWAP>(a, plan, i);
             const int half = b.cols / 2;                   // columns whose operand rows this CTA loads
             const int b0 = b.c0 + half * (int)rank;
+            // rows of the A operand behind the last token are not loaded: what lies in their place gives rows of the
+            // result that nobody reads.  32 of them always: each producer has a part in every stage, or the ring
+            // could go round twice without one of them, whose waits tell phases apart by their parity only
+            const bool token_rows = !SWAP && (MODE != kModeGrads || b.slice >= 0);
+            auto rows_of = [&](int r) { return token_rows ? min(max((plan.n_live - b.m * kTile - 128 * r + 31) / 32 * 32, 32), 128) : 128; };
+            const int a_rows = rows_of((int)rank);
             // the reduction axis innermost: 32 rows a time at least; outermost: boxes of 64 columns
-            const uint32_t bytes = 2 * (kOperandBytes + (MODE != kModeGrads ? half * kBlockK * 2 : (half + 63) / 64 * (64 * kBlockK * 2)));
+            const uint32_t bytes = (uint32_t)(rows_of(0) + rows_of(1)) * kBlockK * 2 + 2 * ((MODE != kModeGrads ? half * kBlockK * 2 : (half + 63) / 64 * (64 * kBlockK * 2)));
             for (int k = b.k0; k < b.k0 + b.ks; ++k) {
                 ok = __all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * s, ph ^ 1u, abort_flag));
                 if (!ok) break;
-                const uint32_t dst = ring + s * kStageBytes + (is_a ? 0 : kOperandBytes);
+                const uint32_t dst = ring + s * stage_bytes + (is_a ? 0 : kOperandBytes);
                 const uint32_t full = full0 + 8 * s;
                 if (elect_one()) {
                     if (is_a) {
                         if (leader) mbar_expect_tx(bar_full + 8 * s, bytes);  // both operands, both CTAs
-                        if (MODE != kModeGrads) tma_load_2d_pair(dst, &maps.x_k, k * kBlockK, b.m * kTile + 128 * (int)rank, full);
-                        else if (b.slice >= 0) tma_load_2d_pair(dst, &maps.g_k, k * kBlockK, b.m * kTile + 128 * (int)rank, full);
+                        if (SWAP) tma_load_2d_pair(dst, &maps.w_k[0], k * kBlockK, a.v0 + b.m * kTile + 128 * (int)rank, full);
+                        else if (token_rows) load_rows(MODE != kModeGrads ? maps.x_k : maps.g_k, dst, k * kBlockK, b.m * kTile + 128 * (int)rank, a_rows, full);
                         else tma_load_3d_pair(dst, &maps.g_mn, 0, k * kBlockK, 4 * b.m + 2 * (int)rank, full);
                     } else if (MODE != kModeGrads) {
-                        int r = 0;
-#pragma unroll
-                        for (int lvl = 0; lvl < 3; ++lvl)
-                            if (half - r >= 128 >> lvl) {
-                                tma_load_2d_pair(dst + r * 128, &maps.w_k[lvl], k * kBlockK, a.v0 + b0 + r, full);
-                                r += 128 >> lvl;
-                            }
+                        load_rows(SWAP ? maps.x_k : maps.w_k, dst, k * kBlockK, (SWAP ? 0 : a.v0) + b0, half, full);
                     } else {
                         const CUtensorMap *m = b.slice >= 0 ? &maps.w_mn : &maps.x_mn;
                         const int k_at = (b.slice >= 0 ? a.v0 : 0) + k * kBlockK;
@@ -345,7 +396,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                     }
                 }
                 __syncwarp();
-                if (++s == kStages) { s = 0; ph ^= 1u; }
+                if (++s == stages) { s = 0; ph ^= 1u; }
             }
         }
         code = 31;
@@ -356,7 +407,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
             while (ok) {
                 const int i = queue.next();
                 if (i < 0) { ok = i == -1; break; }
-                const Block b = block_at<MODE>(a, plan, i);
+                const Block b = block_at<MODE, SWAP>(a, plan, i);
                 if (MODE == kModeGrads && b.slice >= 0 && b.ks == 0) continue;  // an empty slice of a short piece adds nothing
                 const bool a_mn = MODE == kModeGrads && b.slice < 0, b_mn = MODE == kModeGrads;
                 const uint32_t idesc = instr_desc_pair(b.cols) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
@@ -374,7 +425,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                     ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * s, ph, abort_flag));
                     if (!ok) break;
                     tc_fence_after();
-                    const uint64_t da = a0 + (uint64_t)(s * (kStageBytes >> 4)), db = b0 + (uint64_t)(s * (kStageBytes >> 4));
+                    const uint64_t da = a0 + (uint64_t)(s * (stage_bytes >> 4)), db = b0 + (uint64_t)(s * (stage_bytes >> 4));
                     if (elect_one()) {
 #pragma unroll
                         for (int j = 0; j < kBlockK / 16; ++j)
@@ -382,7 +433,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                         umma_commit_pair(bar_empty + 8 * s);
                     }
                     __syncwarp();
-                    if (++s == kStages) { s = 0; ph ^= 1u; }
+                    if (++s == stages) { s = 0; ph ^= 1u; }
                 }
                 if (!ok) break;
                 if (elect_one()) umma_commit_pair(bar_tfull + 8 * buf);
@@ -424,12 +475,14 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
     } else {
         // ------------------------------------------------------------------ epilogue
         const int q = warp & 3;
-        PatchWriter out = {patches + (uint32_t)q * 2 * kStoreBytes, lane, 0};
+        const int ew = warp - 4;
+        // swapped: a patch to turn per warp, then the warps' pairs of half patches to store, or two areas for partial results
+        PatchWriter out = {SWAP ? patches + (uint32_t)(kSwapEpilogueWarps + ew) * kStoreBytes : patches + (uint32_t)q * 2 * kStoreBytes, lane, 0};
         uint32_t count = 0;
         while (ok) {
             const int i = queue.next();
             if (i < 0) { ok = i == -1; break; }
-            const Block b = block_at<MODE>(a, plan, i);
+            const Block b = block_at<MODE, SWAP>(a, plan, i);
             if (MODE == kModeGrads && b.slice >= 0 && b.ks == 0) continue;
             const uint32_t buf = count & 1u, tph = (count >> 1) & 1u;
             ++count;
@@ -437,7 +490,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
             const int v_first = a.v0 + b.c0;                                // logits: vocabulary row of column 0
             int label = -1;
             float lse2 = 0.f, g = 0.f, gl = 0.f;
-            if (MODE != kModeGrads && row < plan.n_live) {
+            if (MODE != kModeGrads && !SWAP && row < plan.n_live) {
                 label = __ldcg(a.row_target + row) - v_first;  // column of the target, if it is one of the block's
                 if (MODE == kModeDl) {
                     lse2 = __ldcg(a.row_lse2 + row);
@@ -454,7 +507,99 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * buf);
             };
-            if (MODE == kModeNll) {
+            if (SWAP) {
+                const uint32_t turn = patches + (uint32_t)ew * kStoreBytes;        // the patch being turned
+                // partial results: [4 quarters][256 tokens] of 8 bytes, twice
+                const uint32_t partial = patches + (uint32_t)kSwapEpilogueWarps * kStoreBytes + (count & 1u) * (4 * kTile * 8);
+                const int vw = a.v0 + b.m * kTile + 128 * (int)rank + 32 * q;      // vocabulary row of this warp's lane 0
+                for (int c0 = 32 * (ew >> 2); c0 < b.cols; c0 += 64) {  // a quarter's two warps take the patches in turn
+                    const int tok = b.c0 + c0 + lane;
+                    const bool live = tok < plan.n_live;
+                    const int rel = live ? ld_ordered(a.row_target + tok) - vw : -1;  // target among the warp's 32 rows?
+                    if (MODE == kModeDl) {
+                        lse2 = live ? __int_as_float(ld_ordered(reinterpret_cast<const int32_t *>(a.row_lse2) + tok)) : 0.f;
+                        g = live ? __int_as_float(ld_ordered(reinterpret_cast<const int32_t *>(a.row_g) + tok)) : 0.f;
+                        gl = live ? __int_as_float(ld_ordered(reinterpret_cast<const int32_t *>(a.row_gl) + tok)) : 0.f;
+                    }
+                    float v[32];
+                    tmem_ld32(t0 + c0, v);
+                    if (c0 + 64 >= b.cols) release();
+#pragma unroll
+                    for (int p = 0; p < 8; ++p)
+                        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(turn + lane * 128 + ((p ^ (lane & 7)) << 4)), "f"(v[4 * p]),
+                                     "f"(v[4 * p + 1]), "f"(v[4 * p + 2]), "f"(v[4 * p + 3]) : "memory");
+                    __syncwarp();
+#pragma unroll
+                    for (int r = 0; r < 32; ++r)
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[r]) : "r"(turn + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) : "memory");
+                    __syncwarp();
+                    const unsigned hit = (unsigned)rel;
+                    if (MODE == kModeNll) {
+                        if (__any_sync(0xffffffffu, hit < 32u)) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (hit == (unsigned)j) {
+                                    a.row_label[tok] = v[j];
+                                    v[j] = -INFINITY;
+                                }
+                        }
+                        if (vw + 32 > a.V) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (vw + j >= a.V) v[j] = -INFINITY;
+                        }
+                        float top = v[0];
+#pragma unroll
+                        for (int j = 1; j < 32; ++j) top = fmaxf(top, v[j]);
+                        const float m2 = top * kLog2e, ref = m2 == -INFINITY ? 0.f : m2;
+                        float s4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) s4[j & 3] += exp2_fast(fmaf(v[j], kLog2e, -ref));
+                        asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(partial + (q * kTile + c0 + lane) * 8), "f"(m2), "f"((s4[0] + s4[1]) + (s4[2] + s4[3])) : "memory");
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = live ? g * exp2_fast(fmaf(v[j], kLog2e, -lse2)) : 0.f;
+                        if (__any_sync(0xffffffffu, hit < 32u)) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (hit == (unsigned)j) v[j] = gl;
+                        }
+                        if (vw + 32 > a.V) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (vw + j >= a.V) v[j] = 0.f;
+                        }
+                        // 32 tokens x 64 bytes, two patches in turn
+                        const uint32_t patch = out.base + (uint32_t)out.turn * (kStoreBytes / 2);
+                        if (lane == 0) bulk_wait_read<1>();
+                        __syncwarp();
+#pragma unroll
+                        for (int p = 0; p < 4; ++p)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(patch + lane * 64 + ((p ^ ((lane >> 1) & 3)) << 4)),
+                                         "r"(pack_bf16(v[8 * p], v[8 * p + 1])), "r"(pack_bf16(v[8 * p + 2], v[8 * p + 3])),
+                                         "r"(pack_bf16(v[8 * p + 4], v[8 * p + 5])), "r"(pack_bf16(v[8 * p + 6], v[8 * p + 7])) : "memory");
+                        out.end([&]() { tma_store_2d(&maps.g_store_32, vw - a.v0, b.c0 + c0, patch); });
+                    }
+                }
+                if (MODE == kModeNll) {  // the four quarters' 32 rows each, of every token
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar_join);
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar_join, (count - 1) & 1u, abort_flag));
+                    if (!ok) break;
+                    for (int c = ew * 32 + lane; c < b.cols; c += 32 * kEpilogue) {
+                        float2 p[4];
+#pragma unroll
+                        for (int w = 0; w < 4; ++w)
+                            asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(p[w].x), "=f"(p[w].y)
+                                         : "r"(partial + (w * kTile + c) * 8) : "memory");
+                        const float top = fmaxf(fmaxf(p[0].x, p[1].x), fmaxf(p[2].x, p[3].x)), ref = top == -INFINITY ? 0.f : top;
+                        float sum = 0.f;
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) sum = fmaf(p[w].y, exp2_fast(p[w].x - ref), sum);
+                        if (b.c0 + c < plan.n_live) a.part[(size_t)(b.c0 + c) * a.part_ld + 2 * b.m + (int)rank] = make_float2(top, sum);
+                    }
+                }
+            } else if (MODE == kModeNll) {
                 float m2 = -INFINITY, sum = 0.f;  // of the logits in units of ln 2, without the target's
                 for (int c0 = 0; c0 < b.cols; c0 += 32) {
                     float v[32];
@@ -488,6 +633,8 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                 if (row < plan.n_live) a.part[(size_t)row * a.part_ld + b.n] = make_float2(m2, sum);
             } else if (MODE == kModeDl) {
                 const bool live = row < plan.n_live;
+                // grad_w reduces over whole steps of 64 tokens: zeros behind the last, and nothing further on
+                if (row - lane >= (plan.n_live + kBlockK - 1) / kBlockK * kBlockK) { release(); continue; }
                 for (int c0 = 0; c0 < b.cols; c0 += 64) {
                     const uint32_t patch = out.begin();
 #pragma unroll
@@ -518,6 +665,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                 }
             } else if (b.slice >= 0) {
                 const int row0 = b.slice * a.dx_pitch + b.m * kTile + 128 * (int)rank + 32 * q;
+                if (row - lane >= plan.n_live) { release(); continue; }
                 for (int c0 = 0; c0 < b.cols; c0 += 32) {
                     const uint32_t patch = out.begin();
                     float v[32];
@@ -698,7 +846,7 @@ vocab_rows_kernel(const RowArgs a, int token_ctas) {
 constexpr int kNllWarps = 8;
 constexpr int kNllBatch = 16;  // partial results that a lane fetches at a time
 __global__ void __launch_bounds__(32 * kNllWarps)
-vocab_nll_kernel(const int32_t *__restrict__ meta, const float2 *__restrict__ part, int part_ld, int V, int n_clusters,
+vocab_nll_kernel(const int32_t *__restrict__ meta, const float2 *__restrict__ part, int part_ld, int V, int n_clusters, bool swap,
                  const int32_t *__restrict__ row_token, const float *__restrict__ row_label, float *__restrict__ nll,
                  float *__restrict__ lse) {
     pdl_launch_dependents();
@@ -707,7 +855,7 @@ vocab_nll_kernel(const int32_t *__restrict__ meta, const float2 *__restrict__ pa
     const int lane = threadIdx.x & 31;
     const int row = blockIdx.x * kNllWarps + (threadIdx.x >> 5);
     if (row >= n_live) return;
-    const int n_vt = logit_blocks(V, (n_live + kTile - 1) / kTile, n_clusters);
+    const int n_vt = swap ? 2 * ((V + kTile - 1) / kTile) : logit_blocks(V, (n_live + kTile - 1) / kTile, n_clusters);
     const float2 *src = part + (size_t)row * part_ld;
     const float at = __ldcg(row_label + row);
     const int t = __ldcg(row_token + row);
@@ -743,6 +891,7 @@ vocab_nll_kernel(const int32_t *__restrict__ meta, const float2 *__restrict__ pa
 }
 
 // grad_x: the slices' sums of a row, rounded, to its token; a warp takes 256 columns
+constexpr int kSliceBatch = 5;  // slices fetched at a time
 __global__ void __launch_bounds__(kRowThreads)
 vocab_grad_x_kernel(const int32_t *__restrict__ meta, const float *__restrict__ dx, int splits, size_t slice_stride, int d,
                     const int32_t *__restrict__ row_token, __nv_bfloat16 *__restrict__ grad_x) {
@@ -757,12 +906,20 @@ vocab_grad_x_kernel(const int32_t *__restrict__ meta, const float *__restrict__ 
         const int t = __ldcg(row_token + r);
         const float *src = dx + (size_t)r * d + c;
         float4 lo = __ldcg(reinterpret_cast<const float4 *>(src)), hi = __ldcg(reinterpret_cast<const float4 *>(src) + 1);
-#pragma unroll 4
-        for (int s = 1; s < splits; ++s) {
-            const float4 *p = reinterpret_cast<const float4 *>(src + s * slice_stride);
-            const float4 l = __ldcg(p), h = __ldcg(p + 1);
-            lo.x += l.x; lo.y += l.y; lo.z += l.z; lo.w += l.w;
-            hi.x += h.x; hi.y += h.y; hi.z += h.z; hi.w += h.w;
+        for (int s0 = 1; s0 < splits; s0 += kSliceBatch) {
+            float4 l[kSliceBatch], h[kSliceBatch];
+#pragma unroll
+            for (int i = 0; i < kSliceBatch; ++i) {  // (behind the last slice: the last again, not added)
+                const float4 *p = reinterpret_cast<const float4 *>(src + min(s0 + i, splits - 1) * slice_stride);
+                l[i] = __ldcg(p);
+                h[i] = __ldcg(p + 1);
+            }
+#pragma unroll
+            for (int i = 0; i < kSliceBatch; ++i)
+                if (s0 + i < splits) {
+                    lo.x += l[i].x; lo.y += l[i].y; lo.z += l[i].z; lo.w += l[i].w;
+                    hi.x += h[i].x; hi.y += h[i].y; hi.z += h[i].z; hi.w += h[i].w;
+                }
         }
         *reinterpret_cast<uint4 *>(grad_x + (size_t)t * d + c) =
             make_uint4(pack_bf16(lo.x, lo.y), pack_bf16(lo.z, lo.w), pack_bf16(hi.x, hi.y), pack_bf16(hi.z, hi.w));
@@ -796,6 +953,13 @@ int grad_x_splits(int T, int d, int kp) {
     return s < 1 ? 1 : s;
 }
 
+// Few tokens are the columns of the logits' blocks, in units of 64, where blocks of 256 token rows would be filled up by a
+// quarter of the tokens or more (up to 192 tokens, 257 to 384, 513 to 576).  Narrower blocks load more bytes per product, and
+// their epilogue turns every patch, so the blocks of rows are level or ahead elsewhere.  us, likelihoods and gradients, rows
+// and columns, of 65,536 x 2048: 64 tokens 61.4 + 191, 53.7 + 182; 300 tokens 101 + 288, 88.2 + 275; 256 tokens 63.5 + 226,
+// 65.9 + 227; 900 tokens 184 + 551, 185 + 579.
+bool tokens_as_columns(int T) { return T <= kSwapTokens && 16 * tiles(T) >= 5 * ((T + 63) / 64); }
+
 size_t vocab_carve(const zeda_vocab_config_t &c, unsigned char *base, zeda_vocab *h) {
     size_t off = 0;
     auto take = [&](size_t bytes) -> void * {
@@ -818,7 +982,9 @@ size_t vocab_carve(const zeda_vocab_config_t &c, unsigned char *base, zeda_vocab
     v.row_target = (int32_t *)take((size_t)v.rows * 4);
     v.row_label = (float *)take((size_t)v.rows * 4);
     v.part_ld = tiles(c.n_vocab) + kMaxClusters;  // (logit_blocks adds less than a turn)
-    v.part = (float2 *)take((size_t)v.part_ld * v.rows * 8);
+    const size_t few_tokens = v.rows < kSwapTokens ? v.rows : kSwapTokens;
+    const size_t part = (size_t)v.part_ld * v.rows, part_swap = 2 * (size_t)tiles(c.n_vocab) * few_tokens;
+    v.part = (float2 *)take((part > part_swap ? part : part_swap) * 8);
     v.xc = (__nv_bfloat16 *)take((size_t)v.rows * c.d_model * 2);
     if (c.backward) {
         v.row_lse2 = (float *)take((size_t)v.rows * 4);
@@ -838,10 +1004,11 @@ size_t vocab_carve(const zeda_vocab_config_t &c, unsigned char *base, zeda_vocab
     return off;
 }
 
-bool map_2d(CUtensorMap *m, const void *base, size_t rows, size_t cols, int box_cols, int box_rows) {
+bool map_2d(CUtensorMap *m, const void *base, size_t rows, size_t cols, int box_cols, int box_rows,
+            CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
     const cuuint64_t dims[2] = {cols, rows}, strides[1] = {cols * 2};
     const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
-    return encode_bf16_map(m, base, 2, dims, strides, box);
+    return encode_bf16_map(m, base, 2, dims, strides, box, swizzle);
 }
 
 // [steps][cols] with the columns in blocks of 64: one box holds 64 steps of two blocks, block after block
@@ -853,11 +1020,14 @@ bool map_mn(CUtensorMap *m, const void *base, size_t steps, size_t cols) {
 
 bool build_maps(zeda_vocab *h, VocabMaps *m) {
     const size_t d = h->cfg.d_model, V = h->cfg.n_vocab;
-    bool ok = map_2d(&m->x_k, h->xc, h->rows, d, kBlockK, 128);
-    for (int i = 0; i < 3; ++i) ok = ok && map_2d(&m->w_k[i], h->w, V, d, kBlockK, 128 >> i);
+    bool ok = true;
+    for (int i = 0; i < 3; ++i)
+        ok = ok && map_2d(&m->x_k[i], h->xc, h->rows, d, kBlockK, 128 >> i) && map_2d(&m->w_k[i], h->w, V, d, kBlockK, 128 >> i);
     if (ok && h->cfg.backward) {
-        ok = map_2d(&m->g_k, h->g, h->rows, h->piece, kBlockK, 128) && map_2d(&m->x_mn, h->xc, h->rows, d, 64, kBlockK) &&
-             map_2d(&m->w_mn, h->w, V, d, 64, kBlockK) && map_mn(&m->g_mn, h->g, h->rows, h->piece) && map_2d(&m->g_store, h->g, h->rows, h->piece, 64, 32);
+        ok = map_2d(&m->x_mn, h->xc, h->rows, d, 64, kBlockK) &&
+             map_2d(&m->w_mn, h->w, V, d, 64, kBlockK) && map_mn(&m->g_mn, h->g, h->rows, h->piece) && map_2d(&m->g_store, h->g, h->rows, h->piece, 64, 32) &&
+             map_2d(&m->g_store_32, h->g, h->rows, h->piece, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+        for (int i = 0; i < 3; ++i) ok = ok && map_2d(&m->g_k[i], h->g, h->rows, h->piece, kBlockK, 128 >> i);
         const cuuint64_t dims[2] = {d, (cuuint64_t)h->dx_rows}, strides[1] = {d * 4};
         const cuuint32_t box[2] = {32, 32};
         ok = ok && encode_f32_map(&m->dx_store, h->dx, 2, dims, strides, box);
@@ -867,9 +1037,9 @@ bool build_maps(zeda_vocab *h, VocabMaps *m) {
 
 int clusters(const zeda_vocab *h) { return h->sm_count / 2 < kMaxClusters ? h->sm_count / 2 : kMaxClusters; }
 
-template <int MODE>
+template <int MODE, bool SWAP>
 cudaError_t launch_gemm(const zeda_vocab *h, const CUtensorMap &map_gw, const GemmArgs &a, cudaStream_t s) {
-    return launch_kernel(h->pdl, vocab_gemm_kernel<MODE>, dim3(2 * clusters(h)), dim3(kGemmThreads), (size_t)kGemmSmem, s,
+    return launch_kernel(h->pdl, vocab_gemm_kernel<MODE, SWAP>, dim3(2 * clusters(h)), dim3(gemm_threads(SWAP)), (size_t)kGemmSmem, s,
                          *static_cast<const VocabMaps *>(h->maps), map_gw, a);
 }
 
@@ -970,8 +1140,9 @@ zeda_status_t zeda_vocab_create(const zeda_vocab_config_t *cfg, const void *w, v
     vocab_carve(*cfg, static_cast<unsigned char *>(workspace), h);
     zeda_status_t st = ZEDA_OK;
     if (!build_maps(h, maps)) st = ZEDA_ERR_CUDA;
-    const void *kernels[3] = {(const void *)vocab_gemm_kernel<kModeNll>, (const void *)vocab_gemm_kernel<kModeDl>,
-                              (const void *)vocab_gemm_kernel<kModeGrads>};
+    const void *kernels[5] = {(const void *)vocab_gemm_kernel<kModeNll, false>, (const void *)vocab_gemm_kernel<kModeNll, true>,
+                              (const void *)vocab_gemm_kernel<kModeDl, false>, (const void *)vocab_gemm_kernel<kModeDl, true>,
+                              (const void *)vocab_gemm_kernel<kModeGrads, false>};
     for (const void *k : kernels)
         if (st == ZEDA_OK && (e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem)) != cudaSuccess)
             st = vocab_fail("kernel set-up", e);
@@ -1004,11 +1175,14 @@ zeda_status_t zeda_vocab_nll(zeda_vocab_t *h, const void *x, const int32_t *targ
     r.nll = nll;
     r.lse = lse;
     if ((e = launch_rows<false>(h, r, s)) != cudaSuccess) return vocab_fail("row gather launch", e);
-    const GemmArgs a = gemm_args(h);
-    const VocabMaps *maps = static_cast<const VocabMaps *>(h->maps);
-    if ((e = launch_gemm<kModeNll>(h, maps->x_k, a, s)) != cudaSuccess) return vocab_fail("logits launch", e);
+    GemmArgs a = gemm_args(h);
+    const bool swap = tokens_as_columns(T);
+    if (swap) a.part_ld = 2 * tiles(h->cfg.n_vocab);
+    const CUtensorMap &none = static_cast<const VocabMaps *>(h->maps)->x_k[0];
+    e = swap ? launch_gemm<kModeNll, true>(h, none, a, s) : launch_gemm<kModeNll, false>(h, none, a, s);
+    if (e != cudaSuccess) return vocab_fail("logits launch", e);
     e = launch_kernel(h->pdl, vocab_nll_kernel, dim3((T + kNllWarps - 1) / kNllWarps), dim3(32 * kNllWarps), 0, s, (const int32_t *)h->meta,
-                      (const float2 *)h->part, h->part_ld, h->cfg.n_vocab, clusters(h), (const int32_t *)h->row_token,
+                      (const float2 *)h->part, a.part_ld, h->cfg.n_vocab, clusters(h), swap, (const int32_t *)h->row_token,
                       (const float *)h->row_label, nll, lse);
     if (e != cudaSuccess) return vocab_fail("likelihood launch", e);
     return ZEDA_OK;
@@ -1062,12 +1236,14 @@ zeda_status_t zeda_vocab_nll_backward(zeda_vocab_t *h, const void *x, const int3
     const int V = h->cfg.n_vocab;
     a.splits = grad_x_splits(T, a.d, V < h->piece ? V : h->piece);
     a.dx_pitch = tiles(T) * kTile;
+    a.back = V <= h->piece;
     for (int v0 = 0; v0 < V; v0 += h->piece) {
         a.v0 = v0;
         a.kp = V - v0 < h->piece ? V - v0 : h->piece;
         a.first = v0 == 0;
-        if ((e = launch_gemm<kModeDl>(h, map_gw, a, s)) != cudaSuccess) return vocab_fail("logits' gradient launch", e);
-        if ((e = launch_gemm<kModeGrads>(h, map_gw, a, s)) != cudaSuccess) return vocab_fail("gradients launch", e);
+        e = tokens_as_columns(T) ? launch_gemm<kModeDl, true>(h, map_gw, a, s) : launch_gemm<kModeDl, false>(h, map_gw, a, s);
+        if (e != cudaSuccess) return vocab_fail("logits' gradient launch", e);
+        if ((e = launch_gemm<kModeGrads, false>(h, map_gw, a, s)) != cudaSuccess) return vocab_fail("gradients launch", e);
     }
     const long long warps = (long long)T * ((a.d + 255) / 256), most = 8 * h->sm_count;
     int ctas = (int)((warps + kRowThreads / 32 - 1) / (kRowThreads / 32) < most ? (warps + kRowThreads / 32 - 1) / (kRowThreads / 32) : most);

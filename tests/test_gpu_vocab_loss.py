@@ -95,6 +95,9 @@ SIZES = [  # T, d, V, ignored
     (1, 64, 1, 0.0), (1, 64, 2, 0.0), (3, 64, 31, 0.0), (2, 128, 256, 0.0), (64, 64, 257, 0.3), (65, 192, 1000, 0.0),
     (255, 320, 511, 0.5), (256, 256, 512, 0.0), (257, 64, 4099, 0.1), (700, 1088, 2003, 0.4), (1, 2048, 20011, 0.0),
     (33, 2048, 9000, 0.0), (1500, 512, 3001, 0.25), (300, 8192, 300, 0.0), (2049, 128, 700, 0.9),
+    # either side of where the tokens change from columns to rows of the logits' blocks
+    (2048, 64, 515, 0.0), (2049, 64, 515, 0.0), (2600, 1088, 4100, 0.3), (3000, 192, 1111, 0.5), (4500, 320, 1, 0.0),
+    (5000, 448, 255, 0.99),
 ]
 
 
@@ -120,7 +123,7 @@ def test_gradients(T, d, V, ignored):
     m.close()
 
 
-@pytest.mark.parametrize("T,V", [(300, 5000), (1, 4097), (513, 2049)])
+@pytest.mark.parametrize("T,V", [(300, 5000), (1, 4097), (513, 2049), (2500, 4500)])
 def test_gradients_over_several_pieces_of_the_vocabulary(T, V):
     from paper_2605_18643_b200 import zeda
     x, w, target, grad = make(T, 128, V, seed=T, ignored=0.2 if T > 1 else 0.0)
@@ -255,6 +258,25 @@ def test_no_result_depends_on_the_call_in_front_graphs_and_streams():
         w.copy_(keep)
         m.check()
         m.close()
+
+
+@pytest.mark.parametrize("T", [1, 30, 64, 130, 250, 300])
+def test_many_calls_whose_row_blocks_are_mostly_empty(T):
+    # half of the CTA pairs have no token of their own then: every role has to keep step all the same
+    from paper_2605_18643_b200 import zeda
+    x, w, target, grad = make(T, 2048, 9000, seed=T)
+    m = zeda.VocabLoss(w, T)
+    want = check(zeda, m, x, w, target, grad)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        for _ in range(5):
+            nll, lse = m.nll(x, target)
+            gx, gw = m.backward(x, target, nll, lse, grad)
+    for _ in range(40):
+        g.replay()
+    m.check()
+    assert all(torch.equal(a, b) for a, b in zip(want, (nll, lse, gx, gw)))
+    m.close()
 
 
 def test_refusals():

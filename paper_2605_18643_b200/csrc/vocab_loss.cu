@@ -52,14 +52,15 @@ constexpr int kTile = 256;                       // rows and columns of a block 
 constexpr int kBlockK = 64;                      // of the reduction axis per ring stage
 constexpr int kOperandBytes = 128 * kBlockK * 2; // one CTA's half of an operand's stage
 constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kStages = 6;
+constexpr int kStages = 5;
 constexpr int kStoreBytes = 4096;                // an epilogue warp's patch of 32 rows x 128 bytes
-constexpr int kEpilogueWarps = 4, kSwapEpilogueWarps = 8;  // the turned patches cost latency: two warps per quarter of TMEM hide it
-constexpr int gemm_threads(bool swap) { return 128 + 32 * (swap ? kSwapEpilogueWarps : kEpilogueWarps); }
-constexpr int kSwapRing = 5 * kStageBytes;       // the swapped form's patches take a stage's room
-constexpr int kSwapPatches = 16 * kStoreBytes;
-constexpr int kGemmSmem = kStages * kStageBytes + 8 * kStoreBytes + 1024;
-static_assert(kSwapRing + kSwapPatches + 1024 == kGemmSmem, "both forms fill the shared memory");
+// Two epilogue warps per quarter of TMEM take its columns in turn: one alone waits for its own loads and exponentials most of
+// the time (8192 tokens, d 256, 32,768 rows: 227 us with four warps, 185 with eight).
+constexpr int kEpilogueWarps = 8;
+constexpr int kGemmThreads = 128 + 32 * kEpilogueWarps;
+constexpr int kRingBytes = kStages * kStageBytes;
+constexpr int kPatchBytes = 2 * kEpilogueWarps * kStoreBytes;
+constexpr int kGemmSmem = kRingBytes + kPatchBytes + 1024;
 constexpr int kRowThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr size_t kPieceBytes = (size_t)256 << 20;  // of dl at a time
@@ -106,12 +107,16 @@ struct Block {
     int slice;       // grad_x: slice of the piece; -1: grad_w
 };
 
-// `units` blocks of 64 columns cut into `n` parts whose widths differ by at most one unit
-__device__ __forceinline__ void cut_columns(Block &b, int units, int n) {
-    const int u0 = (int)((long long)units * b.n / n), u1 = (int)((long long)units * (b.n + 1) / n);
-    b.c0 = 64 * u0;
-    b.cols = 64 * (u1 - u0);
-}
+// `units` cut into n parts whose sizes differ by at most one
+struct Cut {
+    int base, extra;
+    __device__ __forceinline__ void make(int units, int n) {
+        base = n ? units / n : 0;
+        extra = units - base * n;
+    }
+    __device__ __forceinline__ int start(int i) const { return i * base + min(i, extra); }
+    __device__ __forceinline__ int size(int i) const { return base + (i < extra ? 1 : 0); }
+};
 
 // Column blocks of the logits: as many as do not lengthen the longest cluster's list of full-sized ones (65,536 rows of
 // the matrix and one row block on 74 clusters: 296 blocks of 192 or 256 columns, not 256 of 256, so that each cluster
@@ -126,6 +131,11 @@ __host__ __device__ inline int logit_blocks(int kp, int n_rb, int n_clusters) {
 
 struct Plan {  // of one launch
     int n_live, n_rb, n_vt, dt, n_blocks;
+    Cut cols, slices;  // columns in units of 64; the piece's reduction steps
+    __device__ __forceinline__ void place_columns(Block &b) const {
+        b.c0 = 64 * cols.start(b.n);
+        b.cols = 64 * cols.size(b.n);
+    }
 };
 
 // SWAP (few tokens): the vocabulary gives the blocks' rows and the tokens their columns, which come in units of 64.
@@ -138,6 +148,7 @@ __device__ __forceinline__ Plan make_plan(const GemmArgs &a, int n_live, int n_c
         p.n_vt = (a.kp + kTile - 1) / kTile;
         p.n_rb = (n_live + kTile - 1) / kTile;  // here: blocks of columns
         p.n_blocks = p.n_vt * p.n_rb;
+        p.cols.make((n_live + 63) / 64, p.n_rb);
         return p;
     }
     p.n_live = n_live;
@@ -145,6 +156,12 @@ __device__ __forceinline__ Plan make_plan(const GemmArgs &a, int n_live, int n_c
     p.dt = (a.d + kTile - 1) / kTile;
     p.n_vt = MODE == kModeGrads ? (a.kp + kTile - 1) / kTile : logit_blocks(a.kp, p.n_rb, n_clusters);
     p.n_blocks = MODE == kModeGrads ? (a.splits * p.n_rb + p.n_vt) * p.dt : p.n_rb * p.n_vt;
+    if (MODE == kModeGrads) {
+        p.cols.make(a.d / 64, p.dt);
+        p.slices.make((a.kp + kBlockK - 1) / kBlockK, a.splits);
+    } else {
+        p.cols.make((a.kp + 63) / 64, p.n_vt);
+    }
     return p;
 }
 
@@ -155,7 +172,7 @@ __device__ __forceinline__ Block block_at(const GemmArgs &a, const Plan &p, int 
     if (SWAP) {
         b.m = i / p.n_rb;
         b.n = i % p.n_rb;
-        cut_columns(b, (p.n_live + 63) / 64, p.n_rb);
+        p.place_columns(b);
         b.k0 = 0;
         b.ks = a.d / kBlockK;
         b.slice = 0;
@@ -164,7 +181,7 @@ __device__ __forceinline__ Block block_at(const GemmArgs &a, const Plan &p, int 
     if (MODE != kModeGrads) {
         b.n = i / p.n_rb;
         b.m = i % p.n_rb;
-        cut_columns(b, (a.kp + 63) / 64, p.n_vt);
+        p.place_columns(b);
         b.k0 = 0;
         b.ks = a.d / kBlockK;
         b.slice = 0;
@@ -176,9 +193,8 @@ __device__ __forceinline__ Block block_at(const GemmArgs &a, const Plan &p, int 
         b.slice = i / per;
         b.m = (i % per) / p.dt;
         b.n = i % p.dt;
-        const int kb = (a.kp + kBlockK - 1) / kBlockK;
-        b.k0 = (int)((long long)kb * b.slice / a.splits);
-        b.ks = (int)((long long)kb * (b.slice + 1) / a.splits) - b.k0;
+        b.k0 = p.slices.start(b.slice);
+        b.ks = p.slices.size(b.slice);
     } else {
         const int j = i - n_dx;
         b.slice = -1;
@@ -187,7 +203,7 @@ __device__ __forceinline__ Block block_at(const GemmArgs &a, const Plan &p, int 
         b.k0 = 0;
         b.ks = (p.n_live + kBlockK - 1) / kBlockK;
     }
-    cut_columns(b, a.d / 64, p.dt);
+    p.place_columns(b);
     return b;
 }
 
@@ -254,6 +270,68 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 
+// Two fp32 operations per instruction: what the epilogue spends beside its exponentials is issue slots.
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+    uint64_t p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+    return p;
+}
+__device__ __forceinline__ void split_pair(uint64_t p, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p)); }
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+// v[j] <- 2^(v[j] log2(e) - ref)
+__device__ __forceinline__ void exponentials(float (&v)[32], float ref) {
+    const uint64_t scale = pair_of(kLog2e, kLog2e), shift = pair_of(-ref, -ref);
+#pragma unroll
+    for (int j = 0; j < 32; j += 2) {
+        float x, y;
+        split_pair(fma_pair(pair_of(v[j], v[j + 1]), scale, shift), x, y);
+        v[j] = exp2_fast(x);
+        v[j + 1] = exp2_fast(y);
+    }
+}
+
+// logits -> their gradients g exp(l - lse); 0 behind the last token, whatever its logits are
+__device__ __forceinline__ void gradients_of_logits(float (&v)[32], bool live, float lse2, float g) {
+    exponentials(v, lse2);
+    const uint64_t gg = pair_of(g, g);
+#pragma unroll
+    for (int j = 0; j < 32; j += 2) {
+        split_pair(mul_pair(pair_of(v[j], v[j + 1]), gg), v[j], v[j + 1]);
+        if (!live) v[j] = v[j + 1] = 0.f;
+    }
+}
+
+__device__ __forceinline__ float largest(const float (&v)[32]) {
+    float m[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+    for (int j = 4; j < 32; ++j) m[j & 3] = fmaxf(m[j & 3], v[j]);
+    return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+}
+
+__device__ __forceinline__ float total(const float (&v)[32]) {
+    uint64_t s[2] = {pair_of(v[0], v[1]), pair_of(v[2], v[3])};
+#pragma unroll
+    for (int j = 4; j < 32; j += 2) s[(j >> 1) & 1] = add_pair(s[(j >> 1) & 1], pair_of(v[j], v[j + 1]));
+    float lo, hi;
+    split_pair(add_pair(s[0], s[1]), lo, hi);
+    return lo + hi;
+}
+
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&p);
@@ -272,6 +350,14 @@ __device__ __forceinline__ void load_rows(const CUtensorMap (&maps)[3], uint32_t
 
 // One patch of 32 rows x 128 bytes to global memory: lane's row of eight 16-byte pieces into the swizzled layout, then
 // one TMA store (or addition) by one lane.  Two patches per warp: the one before is still being read.
+__device__ __forceinline__ void tmem_load(uint32_t taddr, float (&v)[32]) {
+    uint32_t r[32];
+    tmem_ld32_nowait(taddr, r);
+    tmem_ld_wait_for(r);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+}
+
 struct PatchWriter {
     uint32_t base;  // of this warp's two patches
     int lane, turn;
@@ -297,14 +383,14 @@ struct PatchWriter {
 };
 
 // One CTA per SM, persistent.  Warp 0: TMA of the A operand; warp 2: of B; warp 1: TMEM and, in the leader CTA, the MMAs;
-// warp 3 of the leader CTA: the queue of blocks; warps 4-7: epilogue.  Every wait is bounded; a role that gives up records an
+// warp 3 of the leader CTA: the queue of blocks; warps 4-11: epilogue.  Every wait is bounded; a role that gives up records an
 // error word and the CTA leaves through the common exit.
 //
 // SWAP: with few tokens, blocks of 256 token rows would be mostly empty (601 tokens: 768), so W is the M operand and up to
 // 256 tokens, in units of 64, are the N operand.  A thread then reads 32 tokens' logits of one vocabulary row from TMEM; each
 // 32 x 32 patch goes through shared memory, so that from there on a thread again holds a token's logits.
 template <int MODE, bool SWAP>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(gemm_threads(SWAP), 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant__ CUtensorMap map_gw, const GemmArgs a) {
     pdl_launch_dependents();
     extern __shared__ __align__(1024) unsigned char vocab_smem[];
@@ -314,14 +400,12 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
     __shared__ uint32_t s_tmem_base;
     __shared__ int s_abort, s_prod_seq;
     const uint32_t ring = (smem_u32(vocab_smem) + 1023u) & ~1023u;
-    constexpr int kEpilogue = SWAP ? kSwapEpilogueWarps : kEpilogueWarps;
-    constexpr uint32_t kRing = SWAP ? kSwapRing : kStages * kStageBytes;
-    const uint32_t patches = ring + kRing;
+    const uint32_t patches = ring + kRingBytes;
     const uint32_t bar_full = smem_u32(&bars[0]);                    // used in the leader CTA only
     const uint32_t bar_empty = smem_u32(&bars[kMaxStages]);          // one set per CTA
     const uint32_t bar_tfull = smem_u32(&bars[2 * kMaxStages]);      // one set per CTA
     const uint32_t bar_tempty = smem_u32(&bars[2 * kMaxStages + 2]); // used in the leader CTA only
-    const uint32_t bar_join = smem_u32(&bars[2 * kMaxStages + 4]);   // SWAP: the epilogue warps' partial results are written
+    const uint32_t bar_join = smem_u32(&bars[2 * kMaxStages + 4]);   // the epilogue warps' partial results are written
     const uint32_t bar_qfree = smem_u32(&bars[2 * kMaxStages + 5]);  // used in the leader CTA only
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
@@ -331,9 +415,9 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
         s_abort = 0;
         s_prod_seq = -1;
         for (int i = 0; i < kMaxStages; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(bar_tfull + 8 * i, 1); mbar_init(bar_tempty + 8 * i, 2 * kEpilogue); }
-        mbar_init(bar_join, kEpilogue);
-        for (int i = 0; i < kQueue; ++i) mbar_init(bar_qfree + 8 * i, 2 * (2 + kEpilogue) + 1);  // the queue's readers: producers, epilogue, MMA warp
+        for (int i = 0; i < 2; ++i) { mbar_init(bar_tfull + 8 * i, 1); mbar_init(bar_tempty + 8 * i, 2 * kEpilogueWarps); }
+        mbar_init(bar_join, kEpilogueWarps);
+        for (int i = 0; i < kQueue; ++i) mbar_init(bar_qfree + 8 * i, 2 * (2 + kEpilogueWarps) + 1);  // the queue's readers: producers, epilogue, MMA warp
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -351,7 +435,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
     // narrow column blocks leave room for more stages of the matrix's rows
     const int max_half = SWAP ? min(32 * ((plan.n_live + 63) / 64), 128) : 128;
     const uint32_t stage_bytes = SWAP ? kOperandBytes + max_half * kBlockK * 2 : kStageBytes;
-    const uint32_t stages = SWAP ? min(kRing / stage_bytes, (uint32_t)kMaxStages) : kStages;
+    const uint32_t stages = SWAP ? min((uint32_t)kRingBytes / stage_bytes, (uint32_t)kMaxStages) : kStages;
     bool ok = true;
     int code = 0;
 
@@ -475,32 +559,48 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
     } else {
         // ------------------------------------------------------------------ epilogue
         const int q = warp & 3;
-        const int ew = warp - 4;
+        const int ew = warp - 4, turn_of = ew >> 2;  // its place among the quarter's two warps
         // swapped: a patch to turn per warp, then the warps' pairs of half patches to store, or two areas for partial results
-        PatchWriter out = {SWAP ? patches + (uint32_t)(kSwapEpilogueWarps + ew) * kStoreBytes : patches + (uint32_t)q * 2 * kStoreBytes, lane, 0};
+        PatchWriter out = {SWAP ? patches + (uint32_t)(kEpilogueWarps + ew) * kStoreBytes : patches + (uint32_t)ew * 2 * kStoreBytes, lane, 0};
         uint32_t count = 0;
+        // The next block's number, and what its rows' tokens need, are fetched while a block is worked on.
+        struct Ahead {
+            int i;
+            Block b;
+            int label;          // column of the token's target among the block's
+            float lse2, g, gl;
+        } next;
+        auto look_ahead = [&]() {
+            do {
+                next.i = queue.next();
+                if (next.i < 0) return;
+                next.b = block_at<MODE, SWAP>(a, plan, next.i);
+            } while (MODE == kModeGrads && next.b.slice >= 0 && next.b.ks == 0);  // (nothing comes of an empty slice)
+            const int row = next.b.m * kTile + 128 * (int)rank + 32 * q + lane;
+            next.label = -1;
+            if (MODE != kModeGrads && !SWAP && row < plan.n_live) {
+                next.label = __ldcg(a.row_target + row) - (a.v0 + next.b.c0);
+                if (MODE == kModeDl) {
+                    next.lse2 = __ldcg(a.row_lse2 + row);
+                    next.g = __ldcg(a.row_g + row);
+                    next.gl = __ldcg(a.row_gl + row);
+                }
+            }
+        };
+        look_ahead();
         while (ok) {
-            const int i = queue.next();
-            if (i < 0) { ok = i == -1; break; }
-            const Block b = block_at<MODE, SWAP>(a, plan, i);
-            if (MODE == kModeGrads && b.slice >= 0 && b.ks == 0) continue;
+            if (next.i < 0) { ok = next.i == -1; break; }
+            const Block b = next.b;
+            const int label = next.label;
+            float lse2 = next.lse2, g = next.g, gl = next.gl;
             const uint32_t buf = count & 1u, tph = (count >> 1) & 1u;
             ++count;
             const int row = b.m * kTile + 128 * (int)rank + 32 * q + lane;  // of the block's rows, this thread's
             const int v_first = a.v0 + b.c0;                                // logits: vocabulary row of column 0
-            int label = -1;
-            float lse2 = 0.f, g = 0.f, gl = 0.f;
-            if (MODE != kModeGrads && !SWAP && row < plan.n_live) {
-                label = __ldcg(a.row_target + row) - v_first;  // column of the target, if it is one of the block's
-                if (MODE == kModeDl) {
-                    lse2 = __ldcg(a.row_lse2 + row);
-                    g = __ldcg(a.row_g + row);
-                    gl = __ldcg(a.row_gl + row);
-                }
-            }
             ok = __all_sync(0xffffffffu, mbar_wait(bar_tfull + 8 * buf, tph, abort_flag));
             if (!ok) break;
             tc_fence_after();
+            look_ahead();
             const uint32_t t0 = tmem_base + ((uint32_t)(32 * q) << 16) + buf * kTile;
             auto release = [&]() {  // behind the last read of this accumulator
                 tc_fence_before();
@@ -510,9 +610,9 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
             if (SWAP) {
                 const uint32_t turn = patches + (uint32_t)ew * kStoreBytes;        // the patch being turned
                 // partial results: [4 quarters][256 tokens] of 8 bytes, twice
-                const uint32_t partial = patches + (uint32_t)kSwapEpilogueWarps * kStoreBytes + (count & 1u) * (4 * kTile * 8);
+                const uint32_t partial = patches + (uint32_t)kEpilogueWarps * kStoreBytes + (count & 1u) * (4 * kTile * 8);
                 const int vw = a.v0 + b.m * kTile + 128 * (int)rank + 32 * q;      // vocabulary row of this warp's lane 0
-                for (int c0 = 32 * (ew >> 2); c0 < b.cols; c0 += 64) {  // a quarter's two warps take the patches in turn
+                for (int c0 = 32 * turn_of; c0 < b.cols; c0 += 64) {
                     const int tok = b.c0 + c0 + lane;
                     const bool live = tok < plan.n_live;
                     const int rel = live ? ld_ordered(a.row_target + tok) - vw : -1;  // target among the warp's 32 rows?
@@ -522,7 +622,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                         gl = live ? __int_as_float(ld_ordered(reinterpret_cast<const int32_t *>(a.row_gl) + tok)) : 0.f;
                     }
                     float v[32];
-                    tmem_ld32(t0 + c0, v);
+                    tmem_load(t0 + c0, v);
                     if (c0 + 64 >= b.cols) release();
 #pragma unroll
                     for (int p = 0; p < 8; ++p)
@@ -548,17 +648,11 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                             for (int j = 0; j < 32; ++j)
                                 if (vw + j >= a.V) v[j] = -INFINITY;
                         }
-                        float top = v[0];
-#pragma unroll
-                        for (int j = 1; j < 32; ++j) top = fmaxf(top, v[j]);
-                        const float m2 = top * kLog2e, ref = m2 == -INFINITY ? 0.f : m2;
-                        float s4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) s4[j & 3] += exp2_fast(fmaf(v[j], kLog2e, -ref));
-                        asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(partial + (q * kTile + c0 + lane) * 8), "f"(m2), "f"((s4[0] + s4[1]) + (s4[2] + s4[3])) : "memory");
+                        const float m2 = largest(v) * kLog2e, ref = m2 == -INFINITY ? 0.f : m2;
+                        exponentials(v, ref);
+                        asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(partial + (q * kTile + c0 + lane) * 8), "f"(m2), "f"(total(v)) : "memory");
                     } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = live ? g * exp2_fast(fmaf(v[j], kLog2e, -lse2)) : 0.f;
+                        gradients_of_logits(v, live, lse2, g);
                         if (__any_sync(0xffffffffu, hit < 32u)) {
 #pragma unroll
                             for (int j = 0; j < 32; ++j)
@@ -586,7 +680,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                     if (lane == 0) mbar_arrive(bar_join);
                     ok = __all_sync(0xffffffffu, mbar_wait(bar_join, (count - 1) & 1u, abort_flag));
                     if (!ok) break;
-                    for (int c = ew * 32 + lane; c < b.cols; c += 32 * kEpilogue) {
+                    for (int c = ew * 32 + lane; c < b.cols; c += 32 * kEpilogueWarps) {
                         float2 p[4];
 #pragma unroll
                         for (int w = 0; w < 4; ++w)
@@ -601,12 +695,12 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                 }
             } else if (MODE == kModeNll) {
                 float m2 = -INFINITY, sum = 0.f;  // of the logits in units of ln 2, without the target's
-                for (int c0 = 0; c0 < b.cols; c0 += 32) {
+                auto take = [&](uint32_t (&r)[32], int c0) {  // 32 of the row's logits, fetched
                     float v[32];
-                    tmem_ld32(t0 + c0, v);
-                    if (c0 + 32 == b.cols) release();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
                     const unsigned hit = (unsigned)(label - c0);
-                    if (__any_sync(0xffffffffu, hit < 32u && label < b.cols)) {
+                    if (__any_sync(0xffffffffu, hit < 32u)) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
                             if (hit == (unsigned)j) {
@@ -619,32 +713,54 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                         for (int j = 0; j < 32; ++j)
                             if (v_first + c0 + j >= a.V) v[j] = -INFINITY;
                     }
-                    float top = v[0];
-#pragma unroll
-                    for (int j = 1; j < 32; ++j) top = fmaxf(top, v[j]);
-                    const float m_new = fmaxf(m2, top * kLog2e);
+                    const float m_new = fmaxf(m2, largest(v) * kLog2e);
                     const float ref = m_new == -INFINITY ? 0.f : m_new;
-                    float s4[4] = {sum * exp2_fast(m2 - ref), 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) s4[j & 3] += exp2_fast(fmaf(v[j], kLog2e, -ref));
-                    sum = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                    exponentials(v, ref);
+                    sum = fmaf(sum, exp2_fast(m2 - ref), total(v));
                     m2 = m_new;
+                };
+                uint32_t even[32], odd[32];  // the next 32 come in while these are worked on
+                tmem_ld32_nowait(t0 + 32 * turn_of, even);
+                for (int c0 = 32 * turn_of; c0 < b.cols; c0 += 128) {
+                    tmem_ld_wait_for(even);
+                    const bool more = c0 + 64 < b.cols;
+                    if (more) tmem_ld32_nowait(t0 + c0 + 64, odd);
+                    else release();
+                    take(even, c0);
+                    if (!more) break;
+                    tmem_ld_wait_for(odd);
+                    if (c0 + 128 < b.cols) tmem_ld32_nowait(t0 + c0 + 128, even);
+                    else release();
+                    take(odd, c0 + 64);
                 }
-                if (row < plan.n_live) a.part[(size_t)row * a.part_ld + b.n] = make_float2(m2, sum);
+                // the two warps' halves of the row
+                const uint32_t partial = patches + (count & 1u) * kStoreBytes + (uint32_t)lane * 8;
+                asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(partial + (uint32_t)ew * 256), "f"(m2), "f"(sum) : "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_join);
+                ok = __all_sync(0xffffffffu, mbar_wait(bar_join, (count - 1) & 1u, abort_flag));  // (by all eight: none may arrive twice)
+                if (!ok) break;
+                if (turn_of == 0) {
+                    float m_other, s_other;
+                    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(m_other), "=f"(s_other) : "r"(partial + (uint32_t)(ew + 4) * 256) : "memory");
+                    const float top = fmaxf(m2, m_other), ref = top == -INFINITY ? 0.f : top;
+                    if (row < plan.n_live)
+                        a.part[(size_t)row * a.part_ld + b.n] = make_float2(top, sum * exp2_fast(m2 - ref) + s_other * exp2_fast(m_other - ref));
+                }
             } else if (MODE == kModeDl) {
                 const bool live = row < plan.n_live;
                 // grad_w reduces over whole steps of 64 tokens: zeros behind the last, and nothing further on
                 if (row - lane >= (plan.n_live + kBlockK - 1) / kBlockK * kBlockK) { release(); continue; }
-                for (int c0 = 0; c0 < b.cols; c0 += 64) {
+                if (64 * turn_of >= b.cols) release();
+                for (int c0 = 64 * turn_of; c0 < b.cols; c0 += 128) {
                     const uint32_t patch = out.begin();
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         float v[32];
-                        tmem_ld32(t0 + c0 + 32 * half, v);
-                        if (c0 + 64 == b.cols && half == 1) release();
+                        tmem_load(t0 + c0 + 32 * half, v);
+                        if (c0 + 128 >= b.cols && half == 1) release();
                         const int c = c0 + 32 * half;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = live ? g * exp2_fast(fmaf(v[j], kLog2e, -lse2)) : 0.f;
+                        gradients_of_logits(v, live, lse2, g);
                         const unsigned hit = (unsigned)(label - c);
                         if (__any_sync(0xffffffffu, hit < 32u)) {
 #pragma unroll
@@ -666,11 +782,11 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
             } else if (b.slice >= 0) {
                 const int row0 = b.slice * a.dx_pitch + b.m * kTile + 128 * (int)rank + 32 * q;
                 if (row - lane >= plan.n_live) { release(); continue; }
-                for (int c0 = 0; c0 < b.cols; c0 += 32) {
+                for (int c0 = 32 * turn_of; c0 < b.cols; c0 += 64) {
                     const uint32_t patch = out.begin();
                     float v[32];
-                    tmem_ld32(t0 + c0, v);
-                    if (c0 + 32 == b.cols) release();
+                    tmem_load(t0 + c0, v);
+                    if (c0 + 64 >= b.cols) release();
 #pragma unroll
                     for (int p = 0; p < 8; ++p)
                         out.put(patch, p, make_uint4(__float_as_uint(v[4 * p]), __float_as_uint(v[4 * p + 1]), __float_as_uint(v[4 * p + 2]),
@@ -682,13 +798,14 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                 }
             } else {
                 const int v_row0 = a.v0 + b.m * kTile + 128 * (int)rank + 32 * q;
-                for (int c0 = 0; c0 < b.cols; c0 += 64) {
+                if (64 * turn_of >= b.cols) release();
+                for (int c0 = 64 * turn_of; c0 < b.cols; c0 += 128) {
                     const uint32_t patch = out.begin();
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         float v[32];
-                        tmem_ld32(t0 + c0 + 32 * half, v);
-                        if (c0 + 64 == b.cols && half == 1) release();
+                        tmem_load(t0 + c0 + 32 * half, v);
+                        if (c0 + 128 >= b.cols && half == 1) release();
                         if (b.ks == 0) {  // no token carries loss: nothing was accumulated
 #pragma unroll
                             for (int j = 0; j < 32; ++j) v[j] = 0.f;
@@ -1039,7 +1156,7 @@ int clusters(const zeda_vocab *h) { return h->sm_count / 2 < kMaxClusters ? h->s
 
 template <int MODE, bool SWAP>
 cudaError_t launch_gemm(const zeda_vocab *h, const CUtensorMap &map_gw, const GemmArgs &a, cudaStream_t s) {
-    return launch_kernel(h->pdl, vocab_gemm_kernel<MODE, SWAP>, dim3(2 * clusters(h)), dim3(gemm_threads(SWAP)), (size_t)kGemmSmem, s,
+    return launch_kernel(h->pdl, vocab_gemm_kernel<MODE, SWAP>, dim3(2 * clusters(h)), dim3(kGemmThreads), (size_t)kGemmSmem, s,
                          *static_cast<const VocabMaps *>(h->maps), map_gw, a);
 }
 

@@ -10,7 +10,10 @@
 // All products run on CTA pairs (tcgen05.mma.cta_group::2, 256 x 256 blocks, accumulators in TMEM, two of them, so that a
 // block's epilogue runs under the next block's products), operands by TMA:
 //   nll        X W^T; epilogue: each thread holds a token's 256 logits and leaves their maximum and sum of exponentials
-//              relative to it (8 bytes per token and 256 logits), the target's logit kept apart
+//              relative to it, without the target's (12 bytes per token and 256 logits, with the maximum's place).
+//              The tensor cores' sums lose about 1e-6 of a logit at d 2048 (each of their additions truncates), which
+//              is 1e-5 and more of the likelihood of a likely target: the target's logit, and the largest of the
+//              others where it matters, are summed once more in fp32 on the CUDA cores
 //   gradients  by pieces of the vocabulary: X W^T once more, whose epilogue writes the piece's dl as bf16, then in one
 //              launch dl W (added up in fp32 over the pieces) and dl^T X, whose operands lie with the reduction axis
 //              outermost in memory and are read in that layout (MN-major)
@@ -34,8 +37,10 @@ struct zeda_vocab {
     int dx_rows;   // rows of the fp32 sums of grad_x
     // workspace
     int32_t *meta, *row_token, *row_target;
-    float *row_label, *row_lse2, *row_g, *row_gl;
+    double *row_label;
+    float *row_lse2, *row_g, *row_gl;
     float2 *part;  // [rows][part_ld]: a token's partial results side by side
+    int32_t *part_at;
     int part_ld;
     __nv_bfloat16 *xc, *g;
     float *dx;
@@ -62,6 +67,9 @@ constexpr int kRingBytes = kStages * kStageBytes;
 constexpr int kPatchBytes = 2 * kEpilogueWarps * kStoreBytes;
 constexpr int kGemmSmem = kRingBytes + kPatchBytes + 1024;
 constexpr int kRowThreads = 256;
+// From more than so many dimensions on the largest logit is summed once more: the tensor cores' sums, of d / 16 additions,
+// are off by 5e-8 of the likelihoods at d 256, as sums in fp32 are, and by 1.5e-6 at d 2048, 4.7e-7 those in fp32.
+constexpr int kExactTopDim = 512;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr size_t kPieceBytes = (size_t)256 << 20;  // of dl at a time
 constexpr int kSwapStages = 10;                  // at most, of narrow column blocks
@@ -93,9 +101,9 @@ struct GemmArgs {
     int back;        // blocks of the logits from the last to the first: the matrix's end is what the pass in front left in L2
     int32_t *meta;
     const int32_t *row_target;
-    float *row_label;
     const float *row_lse2, *row_g, *row_gl;
-    float2 *part;
+    float2 *part;    // (largest logit, sum of the exponentials above it)
+    int32_t *part_at;  // the vocabulary row of the largest
     int part_ld;
 };
 
@@ -322,6 +330,18 @@ __device__ __forceinline__ float largest(const float (&v)[32]) {
     for (int j = 4; j < 32; ++j) m[j & 3] = fmaxf(m[j & 3], v[j]);
     return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
+
+// Index of the largest: a maximum over the numbers with their index in the five lowest bits.  Among numbers that agree up to
+// there (2^-18 relative) it is some one of them.  0 if all are -inf (tagged, those are NaN, which a maximum passes over).
+__device__ __forceinline__ int place_of_largest(const float (&v)[32]) {
+    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int j = 0; j < 32; ++j) m[j & 3] = fmaxf(m[j & 3], __int_as_float((__float_as_int(v[j]) & ~31) | j));
+    return __float_as_int(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))) & 31;
+}
+
+// The reference of a set of exponentials: its largest logit in units of ln 2 (0 for an empty set).
+__device__ __forceinline__ float reference_of(float top) { return top == -INFINITY ? 0.f : top * kLog2e; }
 
 __device__ __forceinline__ float total(const float (&v)[32]) {
     uint64_t s[2] = {pair_of(v[0], v[1]), pair_of(v[2], v[3])};
@@ -587,6 +607,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                 }
             }
         };
+        const bool exact_top = a.d > kExactTopDim;
         look_ahead();
         while (ok) {
             if (next.i < 0) { ok = next.i == -1; break; }
@@ -611,6 +632,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                 const uint32_t turn = patches + (uint32_t)ew * kStoreBytes;        // the patch being turned
                 // partial results: [4 quarters][256 tokens] of 8 bytes, twice
                 const uint32_t partial = patches + (uint32_t)kEpilogueWarps * kStoreBytes + (count & 1u) * (4 * kTile * 8);
+                const uint32_t partial_at = patches + (uint32_t)kEpilogueWarps * kStoreBytes + 2 * (4 * kTile * 8) + (count & 1u) * (4 * kTile * 4);
                 const int vw = a.v0 + b.m * kTile + 128 * (int)rank + 32 * q;      // vocabulary row of this warp's lane 0
                 for (int c0 = 32 * turn_of; c0 < b.cols; c0 += 64) {
                     const int tok = b.c0 + c0 + lane;
@@ -638,19 +660,18 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                         if (__any_sync(0xffffffffu, hit < 32u)) {
 #pragma unroll
                             for (int j = 0; j < 32; ++j)
-                                if (hit == (unsigned)j) {
-                                    a.row_label[tok] = v[j];
-                                    v[j] = -INFINITY;
-                                }
+                                if (hit == (unsigned)j) v[j] = -INFINITY;
                         }
                         if (vw + 32 > a.V) {
 #pragma unroll
                             for (int j = 0; j < 32; ++j)
                                 if (vw + j >= a.V) v[j] = -INFINITY;
                         }
-                        const float m2 = largest(v) * kLog2e, ref = m2 == -INFINITY ? 0.f : m2;
-                        exponentials(v, ref);
-                        asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(partial + (q * kTile + c0 + lane) * 8), "f"(m2), "f"(total(v)) : "memory");
+                        const float top = largest(v);
+                        const int at = exact_top ? vw + place_of_largest(v) : 0;
+                        exponentials(v, reference_of(top));
+                        asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(partial + (q * kTile + c0 + lane) * 8), "f"(top), "f"(total(v)) : "memory");
+                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(partial_at + (q * kTile + c0 + lane) * 4), "r"(at) : "memory");
                     } else {
                         gradients_of_logits(v, live, lse2, g);
                         if (__any_sync(0xffffffffu, hit < 32u)) {
@@ -686,15 +707,26 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                         for (int w = 0; w < 4; ++w)
                             asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(p[w].x), "=f"(p[w].y)
                                          : "r"(partial + (w * kTile + c) * 8) : "memory");
-                        const float top = fmaxf(fmaxf(p[0].x, p[1].x), fmaxf(p[2].x, p[3].x)), ref = top == -INFINITY ? 0.f : top;
+                        const float top = fmaxf(fmaxf(p[0].x, p[1].x), fmaxf(p[2].x, p[3].x)), ref = reference_of(top);
                         float sum = 0.f;
+                        int from = 0;
 #pragma unroll
-                        for (int w = 0; w < 4; ++w) sum = fmaf(p[w].y, exp2_fast(p[w].x - ref), sum);
-                        if (b.c0 + c < plan.n_live) a.part[(size_t)(b.c0 + c) * a.part_ld + 2 * b.m + (int)rank] = make_float2(top, sum);
+                        for (int w = 0; w < 4; ++w) {
+                            sum = fmaf(p[w].y, exp2_fast(reference_of(p[w].x) - ref), sum);
+                            if (p[w].x == top) from = w;
+                        }
+                        int at;
+                        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(at) : "r"(partial_at + (from * kTile + c) * 4) : "memory");
+                        if (b.c0 + c < plan.n_live) {
+                            const size_t to = (size_t)(b.c0 + c) * a.part_ld + 2 * b.m + (int)rank;
+                            a.part[to] = make_float2(top, sum);
+                            if (exact_top) a.part_at[to] = at;
+                        }
                     }
                 }
             } else if (MODE == kModeNll) {
-                float m2 = -INFINITY, sum = 0.f;  // of the logits in units of ln 2, without the target's
+                float best = -INFINITY, sum = 0.f;  // of the logits, without the target's
+                int best_at = 0;
                 auto take = [&](uint32_t (&r)[32], int c0) {  // 32 of the row's logits, fetched
                     float v[32];
 #pragma unroll
@@ -703,21 +735,23 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                     if (__any_sync(0xffffffffu, hit < 32u)) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
-                            if (hit == (unsigned)j) {
-                                a.row_label[row] = v[j];
-                                v[j] = -INFINITY;
-                            }
+                            if (hit == (unsigned)j) v[j] = -INFINITY;
                     }
                     if (v_first + c0 + 32 > a.V) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
                             if (v_first + c0 + j >= a.V) v[j] = -INFINITY;
                     }
-                    const float m_new = fmaxf(m2, largest(v) * kLog2e);
-                    const float ref = m_new == -INFINITY ? 0.f : m_new;
+                    const float top = largest(v);
+                    const float ref_before = reference_of(best);
+                    if (exact_top) {
+                        const int at = v_first + c0 + place_of_largest(v);
+                        if (top > best) best_at = at;
+                    }
+                    best = fmaxf(best, top);
+                    const float ref = reference_of(best);
                     exponentials(v, ref);
-                    sum = fmaf(sum, exp2_fast(m2 - ref), total(v));
-                    m2 = m_new;
+                    sum = fmaf(sum, exp2_fast(ref_before - ref), total(v));
                 };
                 uint32_t even[32], odd[32];  // the next 32 come in while these are worked on
                 tmem_ld32_nowait(t0 + 32 * turn_of, even);
@@ -734,18 +768,22 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                     take(odd, c0 + 64);
                 }
                 // the two warps' halves of the row
-                const uint32_t partial = patches + (count & 1u) * kStoreBytes + (uint32_t)lane * 8;
-                asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(partial + (uint32_t)ew * 256), "f"(m2), "f"(sum) : "memory");
+                const uint32_t partial = patches + (count & 1u) * kStoreBytes + (uint32_t)lane * 16;
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %3};" ::"r"(partial + (uint32_t)ew * 512), "r"(__float_as_int(best)),
+                             "r"(__float_as_int(sum)), "r"(best_at) : "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar_join);
                 ok = __all_sync(0xffffffffu, mbar_wait(bar_join, (count - 1) & 1u, abort_flag));  // (by all eight: none may arrive twice)
                 if (!ok) break;
-                if (turn_of == 0) {
-                    float m_other, s_other;
-                    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(m_other), "=f"(s_other) : "r"(partial + (uint32_t)(ew + 4) * 256) : "memory");
-                    const float top = fmaxf(m2, m_other), ref = top == -INFINITY ? 0.f : top;
-                    if (row < plan.n_live)
-                        a.part[(size_t)row * a.part_ld + b.n] = make_float2(top, sum * exp2_fast(m2 - ref) + s_other * exp2_fast(m_other - ref));
+                if (turn_of == 0 && row < plan.n_live) {
+                    int other_top, other_sum, other_at, unused;
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(other_top), "=r"(other_sum), "=r"(other_at), "=r"(unused)
+                                 : "r"(partial + (uint32_t)(ew + 4) * 512) : "memory");
+                    const float top2 = __int_as_float(other_top), top = fmaxf(best, top2), ref = reference_of(top);
+                    const size_t to = (size_t)row * a.part_ld + b.n;
+                    a.part[to] = make_float2(top, fmaf(sum, exp2_fast(reference_of(best) - ref),
+                                                       __int_as_float(other_sum) * exp2_fast(reference_of(top2) - ref)));
+                    if (exact_top) a.part_at[to] = top2 > best ? other_at : best_at;
                 }
             } else if (MODE == kModeDl) {
                 const bool live = row < plan.n_live;
@@ -837,12 +875,34 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
     }
 }
 
+// Products of bf16 numbers are exact in fp32; eight at a time are added in fp32, the eights in 64 bits: one fp32 number would be
+// off by 1e-6 for a logit of 18, and a likelihood is a difference of two such.
+__device__ __forceinline__ float dot8(uint4 x, uint4 w) {
+    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ws[4] = {w.x, w.y, w.z, w.w};
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        s = fmaf(__uint_as_float(xs[k] << 16), __uint_as_float(ws[k] << 16), s);
+        s = fmaf(__uint_as_float(xs[k] & 0xffff0000u), __uint_as_float(ws[k] & 0xffff0000u), s);
+    }
+    return s;
+}
+
+template <typename F>
+__device__ __forceinline__ F warp_total(F v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
 struct RowArgs {
     const __nv_bfloat16 *x;
     const int32_t *target;
     int T, V, d;
     __nv_bfloat16 *xc;
     int32_t *meta, *row_token, *row_target;
+    const __nv_bfloat16 *w;                        // forward: the targets' logits
+    double *row_label;
     float *nll, *lse;                              // forward: zeros for tokens without a target
     const float *nll_in, *lse_in, *grad_in;        // backward
     float *row_lse2, *row_g, *row_gl;
@@ -860,7 +920,7 @@ __global__ void __launch_bounds__(kRowThreads)
 vocab_rows_kernel(const RowArgs a, int token_ctas) {
     pdl_launch_dependents();
     __shared__ int s_sum[3][kRowThreads / 32];
-    __shared__ int s_row[kRowThreads];
+    __shared__ int s_row[kRowThreads], s_target[kRowThreads];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     constexpr int kWarps = kRowThreads / 32;
     const int share = (a.T + token_ctas - 1) / token_ctas;
@@ -868,16 +928,27 @@ vocab_rows_kernel(const RowArgs a, int token_ctas) {
     const int chunks = a.d / 8;
     pdl_wait();
     if (blockIdx.x == 0 && tid == 0) a.meta[kNextBlock] = 0;
-    auto fetch = [&](int t, int c0, uint4 (&v)[kRowChunks]) {
-        const uint4 *src = reinterpret_cast<const uint4 *>(a.x + (size_t)t * a.d);
+    auto live = [&](int target) { return (unsigned)target < (unsigned)a.V; };
+    auto fetch = [&](const __nv_bfloat16 *m, int t, int c0, uint4 (&v)[kRowChunks]) {
+        const uint4 *src = reinterpret_cast<const uint4 *>(m + (size_t)t * a.d);
 #pragma unroll
         for (int i = 0; i < kRowChunks; ++i)
             if (c0 + 32 * i + lane < chunks) v[i] = __ldcg(src + c0 + 32 * i + lane);
     };
-    auto live = [&](int target) { return (unsigned)target < (unsigned)a.V; };
-    uint4 v[kRowChunks];
+    auto dot = [&](const uint4 (&x)[kRowChunks], const uint4 (&w)[kRowChunks], int c0) {
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < kRowChunks; ++i)
+            if (c0 + 32 * i + lane < chunks) sum += (double)dot8(x[i], w[i]);
+        return sum;
+    };
+    uint4 v[kRowChunks], wv[kRowChunks];
     int target = t0 + tid < t1 ? __ldcg(a.target + t0 + tid) : -1;
-    if (t0 + warp < t1) fetch(t0 + warp, 0, v);
+    if (t0 + warp < t1) {
+        const int mine = BACKWARD ? -1 : __ldcg(a.target + t0 + warp);
+        fetch(a.x, t0 + warp, 0, v);
+        if (!BACKWARD && live(mine)) fetch(a.w, mine, 0, wv);
+    }
     int before = 0, total = 0;
     for (int base = tid; base < a.T; base += kRowThreads * kRowTargets) {
         float f[kRowTargets];
@@ -915,6 +986,7 @@ vocab_rows_kernel(const RowArgs a, int token_ctas) {
             before += s_sum[2][w];
         }
         s_row[tid] = on ? row : -1;
+        s_target[tid] = target;
         if (t < t1) {
             if (on) {
                 a.row_token[row] = t;
@@ -933,6 +1005,7 @@ vocab_rows_kernel(const RowArgs a, int token_ctas) {
         __syncthreads();
         for (int i = warp; i < min(kRowThreads, t1 - sub); i += kWarps) {
             const int r = s_row[i];
+            double logit = 0.0;
             uint4 *dst = reinterpret_cast<uint4 *>(r >= 0 ? a.xc + (size_t)r * a.d : a.grad_x + (size_t)(sub + i) * a.d);
             for (int c0 = 0; c0 < chunks; c0 += 32 * kRowChunks) {
                 if (r < 0) {
@@ -940,11 +1013,17 @@ vocab_rows_kernel(const RowArgs a, int token_ctas) {
 #pragma unroll
                     for (int k = 0; k < kRowChunks; ++k) v[k] = make_uint4(0, 0, 0, 0);
                 } else if (sub > t0 || i != warp || c0 > 0) {
-                    fetch(sub + i, c0, v);
+                    fetch(a.x, sub + i, c0, v);
+                    if (!BACKWARD) fetch(a.w, s_target[i], c0, wv);
                 }
 #pragma unroll
                 for (int k = 0; k < kRowChunks; ++k)
                     if (c0 + 32 * k + lane < chunks) dst[c0 + 32 * k + lane] = v[k];
+                if (!BACKWARD) logit += dot(v, wv, c0);
+            }
+            if (!BACKWARD && r >= 0) {
+                logit = warp_total(logit);
+                if (lane == 0) a.row_label[r] = logit;
             }
         }
     }
@@ -958,28 +1037,39 @@ vocab_rows_kernel(const RowArgs a, int token_ctas) {
     }
 }
 
-// The partial maxima and sums of a token's logits, and its likelihood: a warp a row.  The target's logit was kept apart:
-// nll = log(1 + sum of the others' exp(l - l_target)) keeps its digits where the target is nearly certain.
+// The partial results of a token's logits, and its likelihood: a warp a row.  The target's logit was kept apart:
+// nll = log(1 + sum of the others' exp(l - l_target)) keeps its digits where the target is nearly certain.  Where the
+// largest of the others has a part in it, that one is summed once more.
 constexpr int kNllWarps = 8;
 constexpr int kNllBatch = 16;  // partial results that a lane fetches at a time
+struct NllArgs {
+    const int32_t *meta;
+    const float2 *part;
+    const int32_t *part_at;
+    int part_ld, V, d, n_clusters;
+    bool swap;
+    const __nv_bfloat16 *xc, *w;
+    const int32_t *row_token;
+    const double *row_label;
+    float *nll, *lse;
+};
 __global__ void __launch_bounds__(32 * kNllWarps)
-vocab_nll_kernel(const int32_t *__restrict__ meta, const float2 *__restrict__ part, int part_ld, int V, int n_clusters, bool swap,
-                 const int32_t *__restrict__ row_token, const float *__restrict__ row_label, float *__restrict__ nll,
-                 float *__restrict__ lse) {
+vocab_nll_kernel(const NllArgs a) {
     pdl_launch_dependents();
     pdl_wait();
-    const int n_live = __ldcg(meta + kLive);
+    const int n_live = __ldcg(a.meta + kLive);
     const int lane = threadIdx.x & 31;
     const int row = blockIdx.x * kNllWarps + (threadIdx.x >> 5);
     if (row >= n_live) return;
-    const int n_vt = swap ? 2 * ((V + kTile - 1) / kTile) : logit_blocks(V, (n_live + kTile - 1) / kTile, n_clusters);
-    const float2 *src = part + (size_t)row * part_ld;
-    const float at = __ldcg(row_label + row);
-    const int t = __ldcg(row_token + row);
-    float m = -INFINITY, sum = 0.f;
+    const int n_vt = a.swap ? 2 * ((a.V + kTile - 1) / kTile) : logit_blocks(a.V, (n_live + kTile - 1) / kTile, a.n_clusters);
+    const float2 *src = a.part + (size_t)row * a.part_ld;
+    const double at = __ldcg(a.row_label + row);
+    const int t = __ldcg(a.row_token + row);
+    float top = -INFINITY, sum = 0.f;
+    int where = -1;
     for (int b0 = lane; b0 < n_vt; b0 += 32 * kNllBatch) {
         float pm[kNllBatch], ps[kNllBatch];
-        float top = m;
+        const float ref_before = reference_of(top);
 #pragma unroll
         for (int i = 0; i < kNllBatch; ++i) {
             const int b = b0 + 32 * i;
@@ -987,24 +1077,44 @@ vocab_nll_kernel(const int32_t *__restrict__ meta, const float2 *__restrict__ pa
             ps[i] = ldcg_if(b < n_vt, reinterpret_cast<const float *>(src + b) + 1, 0.f);
         }
 #pragma unroll
-        for (int i = 0; i < kNllBatch; ++i) top = fmaxf(top, pm[i]);
-        const float ref = top == -INFINITY ? 0.f : top;
-        sum *= exp2_fast(m - ref);
+        for (int i = 0; i < kNllBatch; ++i)
+            if (pm[i] > top) { top = pm[i]; where = b0 + 32 * i; }
+        const float ref = reference_of(top);
+        sum *= exp2_fast(ref_before - ref);
 #pragma unroll
-        for (int i = 0; i < kNllBatch; ++i) sum = fmaf(ps[i], exp2_fast(pm[i] - ref), sum);
-        m = top;
+        for (int i = 0; i < kNllBatch; ++i) sum = fmaf(ps[i], exp2_fast(reference_of(pm[i]) - ref), sum);
     }
-    float top = m;
+    const float own = top;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    sum *= exp2_fast(m - (top == -INFINITY ? 0.f : top));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float ref = reference_of(top);
+    sum = warp_total(sum * exp2_fast(reference_of(own) - ref));
+    if (a.d > kExactTopDim) {
+        const float e_top = exp2_fast(fmaf(top, kLog2e, -ref));  // its part of the sum
+        const unsigned holders = __ballot_sync(0xffffffffu, own == top && where >= 0);
+        if (holders && e_top * 64.f > sum + exp2f(fmaf((float)at, kLog2e, -ref))) {
+            where = __shfl_sync(0xffffffffu, where, __ffs(holders) - 1);
+            const uint4 *x = reinterpret_cast<const uint4 *>(a.xc + (size_t)row * a.d);
+            const uint4 *w = reinterpret_cast<const uint4 *>(a.w + (size_t)__ldcg(a.part_at + (size_t)row * a.part_ld + where) * a.d);
+            double again = 0.0;
+#pragma unroll 8
+            for (int c = lane; c < a.d / 8; c += 32) again += (double)dot8(__ldcg(x + c), __ldcg(w + c));
+            sum = fmaxf(sum - e_top, 0.f) + e_top * exp2f((float)(warp_total(again) - (double)top) * kLog2e);
+        }
+    }
     if (lane != 0) return;
-    const float ahead = fmaf(at, -kLog2e, top);  // of the others' largest logit, in units of ln 2
-    const float loss = ahead > 0.f ? (ahead + log2f(sum + exp2f(-ahead))) * kLn2 : log1pf(sum * exp2f(ahead));
-    nll[t] = loss;
-    lse[t] = at + loss;
+    if (top == -INFINITY) {  // no other row has a part in it
+        a.nll[t] = sum;      // (0, or NaN)
+        a.lse[t] = (float)at;
+        return;
+    }
+    // the others' reference ahead of the target's logit, in units of ln 2: as a sum of two numbers, its exponential as a product
+    const double ahead = (double)ref - at * 1.4426950408889634;
+    const float hi = (float)ahead, lo = (float)(ahead - (double)hi) * kLn2;
+    const double loss = ahead > 0.0 ? (ahead + (double)log2f(sum + exp2f(-hi) * (1.f - lo))) * 0.6931471805599453
+                                    : (double)log1pf(sum * exp2f(hi) * (1.f + lo));
+    a.nll[t] = (float)loss;
+    a.lse[t] = (float)(at + loss);
 }
 
 // grad_x: the slices' sums of a row, rounded, to its token; a warp takes 256 columns
@@ -1097,11 +1207,12 @@ size_t vocab_carve(const zeda_vocab_config_t &c, unsigned char *base, zeda_vocab
     v.meta = (int32_t *)take(kVocabMetaCount * 4);
     v.row_token = (int32_t *)take((size_t)v.rows * 4);
     v.row_target = (int32_t *)take((size_t)v.rows * 4);
-    v.row_label = (float *)take((size_t)v.rows * 4);
+    v.row_label = (double *)take((size_t)v.rows * 8);
     v.part_ld = tiles(c.n_vocab) + kMaxClusters;  // (logit_blocks adds less than a turn)
     const size_t few_tokens = v.rows < kSwapTokens ? v.rows : kSwapTokens;
     const size_t part = (size_t)v.part_ld * v.rows, part_swap = 2 * (size_t)tiles(c.n_vocab) * few_tokens;
     v.part = (float2 *)take((part > part_swap ? part : part_swap) * 8);
+    if (c.d_model > kExactTopDim) v.part_at = (int32_t *)take((part > part_swap ? part : part_swap) * 4);
     v.xc = (__nv_bfloat16 *)take((size_t)v.rows * c.d_model * 2);
     if (c.backward) {
         v.row_lse2 = (float *)take((size_t)v.rows * 4);
@@ -1184,11 +1295,11 @@ GemmArgs gemm_args(const zeda_vocab *h) {
     a.kp = h->cfg.n_vocab;
     a.meta = h->meta;
     a.row_target = h->row_target;
-    a.row_label = h->row_label;
     a.row_lse2 = h->row_lse2;
     a.row_g = h->row_g;
     a.row_gl = h->row_gl;
     a.part = h->part;
+    a.part_at = h->part_at;
     a.part_ld = h->part_ld;
     return a;
 }
@@ -1237,9 +1348,12 @@ zeda_status_t zeda_vocab_create(const zeda_vocab_config_t *cfg, const void *w, v
     if (e != cudaSuccess) return vocab_fail("cudaGetDeviceCount", e);
     if (cfg->device < 0 || cfg->device >= ndev) { set_error("device %d not present (%d devices)", cfg->device, ndev); return ZEDA_ERR_INVALID_ARG; }
     if ((e = cudaSetDevice(cfg->device)) != cudaSuccess) return vocab_fail("cudaSetDevice", e);
-    cudaDeviceProp prop;
-    if ((e = cudaGetDeviceProperties(&prop, cfg->device)) != cudaSuccess) return vocab_fail("cudaGetDeviceProperties", e);
-    if (prop.major != 10) { set_error("this library is built for sm_100a only; device is sm_%d%d", prop.major, prop.minor); return ZEDA_ERR_UNSUPPORTED; }
+    int major = 0, minor = 0, sms = 0;  // (the whole of cudaGetDeviceProperties takes a millisecond)
+    e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, cfg->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, cfg->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, cfg->device);
+    if (e != cudaSuccess) return vocab_fail("cudaDeviceGetAttribute", e);
+    if (major != 10) { set_error("this library is built for sm_100a only; device is sm_%d%d", major, minor); return ZEDA_ERR_UNSUPPORTED; }
     zeda_vocab *h = new (std::nothrow) zeda_vocab();
     VocabMaps *maps = static_cast<VocabMaps *>(aligned_alloc(64, sizeof(VocabMaps)));
     if (!h || !maps) {
@@ -1251,7 +1365,7 @@ zeda_status_t zeda_vocab_create(const zeda_vocab_config_t *cfg, const void *w, v
     memset(maps, 0, sizeof *maps);
     h->cfg = *cfg;
     h->pdl = !(cfg->flags & ZEDA_FLAG_NO_DEPENDENT_LAUNCH);
-    h->sm_count = prop.multiProcessorCount;
+    h->sm_count = sms;
     h->w = static_cast<const __nv_bfloat16 *>(w);
     h->maps = maps;
     vocab_carve(*cfg, static_cast<unsigned char *>(workspace), h);
@@ -1289,6 +1403,8 @@ zeda_status_t zeda_vocab_nll(zeda_vocab_t *h, const void *x, const int32_t *targ
     r.x = static_cast<const __nv_bfloat16 *>(x);
     r.target = target;
     r.T = T;
+    r.w = h->w;
+    r.row_label = h->row_label;
     r.nll = nll;
     r.lse = lse;
     if ((e = launch_rows<false>(h, r, s)) != cudaSuccess) return vocab_fail("row gather launch", e);
@@ -1298,9 +1414,8 @@ zeda_status_t zeda_vocab_nll(zeda_vocab_t *h, const void *x, const int32_t *targ
     const CUtensorMap &none = static_cast<const VocabMaps *>(h->maps)->x_k[0];
     e = swap ? launch_gemm<kModeNll, true>(h, none, a, s) : launch_gemm<kModeNll, false>(h, none, a, s);
     if (e != cudaSuccess) return vocab_fail("logits launch", e);
-    e = launch_kernel(h->pdl, vocab_nll_kernel, dim3((T + kNllWarps - 1) / kNllWarps), dim3(32 * kNllWarps), 0, s, (const int32_t *)h->meta,
-                      (const float2 *)h->part, a.part_ld, h->cfg.n_vocab, clusters(h), swap, (const int32_t *)h->row_token,
-                      (const float *)h->row_label, nll, lse);
+    const NllArgs n = {h->meta, h->part, h->part_at, a.part_ld, h->cfg.n_vocab, a.d, clusters(h), swap, h->xc, h->w, h->row_token, h->row_label, nll, lse};
+    e = launch_kernel(h->pdl, vocab_nll_kernel, dim3((T + kNllWarps - 1) / kNllWarps), dim3(32 * kNllWarps), 0, s, n);
     if (e != cudaSuccess) return vocab_fail("likelihood launch", e);
     return ZEDA_OK;
 }

@@ -57,15 +57,16 @@ constexpr int kTile = 256;                       // rows and columns of a block 
 constexpr int kBlockK = 64;                      // of the reduction axis per ring stage
 constexpr int kOperandBytes = 128 * kBlockK * 2; // one CTA's half of an operand's stage
 constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kStages = 5;
+constexpr int kStages = 6, kSwapFullStages = 5;  // the swapped form's patches take a stage's room
 constexpr int kStoreBytes = 4096;                // an epilogue warp's patch of 32 rows x 128 bytes
 // Two epilogue warps per quarter of TMEM take its columns in turn: one alone waits for its own loads and exponentials most of
 // the time (8192 tokens, d 256, 32,768 rows: 227 us with four warps, 185 with eight).
 constexpr int kEpilogueWarps = 8;
 constexpr int kGemmThreads = 128 + 32 * kEpilogueWarps;
-constexpr int kRingBytes = kStages * kStageBytes;
-constexpr int kPatchBytes = 2 * kEpilogueWarps * kStoreBytes;
+constexpr int kRingBytes = kStages * kStageBytes, kSwapRingBytes = kSwapFullStages * kStageBytes;
+constexpr int kPatchBytes = kEpilogueWarps * kStoreBytes, kSwapPatchBytes = 2 * kEpilogueWarps * kStoreBytes;
 constexpr int kGemmSmem = kRingBytes + kPatchBytes + 1024;
+static_assert(kSwapRingBytes + kSwapPatchBytes + 1024 == kGemmSmem, "both forms fill the shared memory");
 constexpr int kRowThreads = 256;
 // From more than so many dimensions on the largest logit is summed once more: the tensor cores' sums, of d / 16 additions,
 // are off by 5e-8 of the likelihoods at d 256, as sums in fp32 are, and by 1.5e-6 at d 2048, 4.7e-7 those in fp32.
@@ -368,8 +369,6 @@ __device__ __forceinline__ void load_rows(const CUtensorMap (&maps)[3], uint32_t
         }
 }
 
-// One patch of 32 rows x 128 bytes to global memory: lane's row of eight 16-byte pieces into the swizzled layout, then
-// one TMA store (or addition) by one lane.  Two patches per warp: the one before is still being read.
 __device__ __forceinline__ void tmem_load(uint32_t taddr, float (&v)[32]) {
     uint32_t r[32];
     tmem_ld32_nowait(taddr, r);
@@ -378,27 +377,28 @@ __device__ __forceinline__ void tmem_load(uint32_t taddr, float (&v)[32]) {
     for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
 }
 
+// One patch of 32 rows x 128 bytes to global memory: lane's row of eight 16-byte pieces into the swizzled layout, then
+// one TMA store (or addition) by one lane.  One patch per warp: the store before has read it by the time that the next
+// one's numbers are there (a second patch would cost the ring a stage).
 struct PatchWriter {
-    uint32_t base;  // of this warp's two patches
-    int lane, turn;
-    __device__ __forceinline__ uint32_t begin() {
-        if (lane == 0) bulk_wait_read<1>();
+    uint32_t patch;
+    int lane;
+    __device__ __forceinline__ void begin() const {
+        if (lane == 0) bulk_wait_read<0>();
         __syncwarp();
-        return base + (uint32_t)turn * kStoreBytes;
     }
-    __device__ __forceinline__ void put(uint32_t patch, int piece, uint4 v) const {
+    __device__ __forceinline__ void put(int piece, uint4 v) const {
         const uint32_t at = patch + lane * 128 + ((piece ^ (lane & 7)) << 4);
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
     }
     template <typename F>
-    __device__ __forceinline__ void end(F &&issue) {
+    __device__ __forceinline__ void end(F &&issue) const {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) {
             issue();
             bulk_commit();
         }
-        turn ^= 1;
     }
 };
 
@@ -420,7 +420,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
     __shared__ uint32_t s_tmem_base;
     __shared__ int s_abort, s_prod_seq;
     const uint32_t ring = (smem_u32(vocab_smem) + 1023u) & ~1023u;
-    const uint32_t patches = ring + kRingBytes;
+    const uint32_t patches = ring + (SWAP ? kSwapRingBytes : kRingBytes);
     const uint32_t bar_full = smem_u32(&bars[0]);                    // used in the leader CTA only
     const uint32_t bar_empty = smem_u32(&bars[kMaxStages]);          // one set per CTA
     const uint32_t bar_tfull = smem_u32(&bars[2 * kMaxStages]);      // one set per CTA
@@ -455,7 +455,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
     // narrow column blocks leave room for more stages of the matrix's rows
     const int max_half = SWAP ? min(32 * ((plan.n_live + 63) / 64), 128) : 128;
     const uint32_t stage_bytes = SWAP ? kOperandBytes + max_half * kBlockK * 2 : kStageBytes;
-    const uint32_t stages = SWAP ? min((uint32_t)kRingBytes / stage_bytes, (uint32_t)kMaxStages) : kStages;
+    const uint32_t stages = SWAP ? min((uint32_t)kSwapRingBytes / stage_bytes, (uint32_t)kMaxStages) : kStages;
     bool ok = true;
     int code = 0;
 
@@ -581,7 +581,8 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
         const int q = warp & 3;
         const int ew = warp - 4, turn_of = ew >> 2;  // its place among the quarter's two warps
         // swapped: a patch to turn per warp, then the warps' pairs of half patches to store, or two areas for partial results
-        PatchWriter out = {SWAP ? patches + (uint32_t)(kEpilogueWarps + ew) * kStoreBytes : patches + (uint32_t)ew * 2 * kStoreBytes, lane, 0};
+        const PatchWriter out = {patches + (uint32_t)(SWAP ? kEpilogueWarps + ew : ew) * kStoreBytes, lane};
+        uint32_t half_patch = 0;  // swapped: of the two, the next to be written
         uint32_t count = 0;
         // The next block's number, and what its rows' tokens need, are fetched while a block is worked on.
         struct Ahead {
@@ -685,7 +686,8 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                                 if (vw + j >= a.V) v[j] = 0.f;
                         }
                         // 32 tokens x 64 bytes, two patches in turn
-                        const uint32_t patch = out.base + (uint32_t)out.turn * (kStoreBytes / 2);
+                        const uint32_t patch = out.patch + half_patch * (kStoreBytes / 2);
+                        half_patch ^= 1u;
                         if (lane == 0) bulk_wait_read<1>();
                         __syncwarp();
 #pragma unroll
@@ -791,7 +793,6 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                 if (row - lane >= (plan.n_live + kBlockK - 1) / kBlockK * kBlockK) { release(); continue; }
                 if (64 * turn_of >= b.cols) release();
                 for (int c0 = 64 * turn_of; c0 < b.cols; c0 += 128) {
-                    const uint32_t patch = out.begin();
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         float v[32];
@@ -810,35 +811,35 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                             for (int j = 0; j < 32; ++j)
                                 if (v_first + c + j >= a.V) v[j] = 0.f;
                         }
+                        if (half == 0) out.begin();
 #pragma unroll
                         for (int p = 0; p < 4; ++p)
-                            out.put(patch, 4 * half + p, make_uint4(pack_bf16(v[8 * p], v[8 * p + 1]), pack_bf16(v[8 * p + 2], v[8 * p + 3]),
+                            out.put(4 * half + p, make_uint4(pack_bf16(v[8 * p], v[8 * p + 1]), pack_bf16(v[8 * p + 2], v[8 * p + 3]),
                                                                     pack_bf16(v[8 * p + 4], v[8 * p + 5]), pack_bf16(v[8 * p + 6], v[8 * p + 7])));
                     }
-                    out.end([&]() { tma_store_2d(&maps.g_store, b.c0 + c0, b.m * kTile + 128 * (int)rank + 32 * q, patch); });
+                    out.end([&]() { tma_store_2d(&maps.g_store, b.c0 + c0, b.m * kTile + 128 * (int)rank + 32 * q, out.patch); });
                 }
             } else if (b.slice >= 0) {
                 const int row0 = b.slice * a.dx_pitch + b.m * kTile + 128 * (int)rank + 32 * q;
                 if (row - lane >= plan.n_live) { release(); continue; }
                 for (int c0 = 32 * turn_of; c0 < b.cols; c0 += 64) {
-                    const uint32_t patch = out.begin();
                     float v[32];
                     tmem_load(t0 + c0, v);
                     if (c0 + 64 >= b.cols) release();
+                    out.begin();
 #pragma unroll
                     for (int p = 0; p < 8; ++p)
-                        out.put(patch, p, make_uint4(__float_as_uint(v[4 * p]), __float_as_uint(v[4 * p + 1]), __float_as_uint(v[4 * p + 2]),
+                        out.put(p, make_uint4(__float_as_uint(v[4 * p]), __float_as_uint(v[4 * p + 1]), __float_as_uint(v[4 * p + 2]),
                                                      __float_as_uint(v[4 * p + 3])));
                     out.end([&]() {
-                        if (a.first) tma_store_2d(&maps.dx_store, b.c0 + c0, row0, patch);
-                        else tma_add_2d(&maps.dx_store, b.c0 + c0, row0, patch);
+                        if (a.first) tma_store_2d(&maps.dx_store, b.c0 + c0, row0, out.patch);
+                        else tma_add_2d(&maps.dx_store, b.c0 + c0, row0, out.patch);
                     });
                 }
             } else {
                 const int v_row0 = a.v0 + b.m * kTile + 128 * (int)rank + 32 * q;
                 if (64 * turn_of >= b.cols) release();
                 for (int c0 = 64 * turn_of; c0 < b.cols; c0 += 128) {
-                    const uint32_t patch = out.begin();
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         float v[32];
@@ -848,13 +849,14 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
 #pragma unroll
                             for (int j = 0; j < 32; ++j) v[j] = 0.f;
                         }
+                        if (half == 0) out.begin();
 #pragma unroll
                         for (int p = 0; p < 4; ++p)
-                            out.put(patch, 4 * half + p, make_uint4(pack_bf16(v[8 * p], v[8 * p + 1]), pack_bf16(v[8 * p + 2], v[8 * p + 3]),
+                            out.put(4 * half + p, make_uint4(pack_bf16(v[8 * p], v[8 * p + 1]), pack_bf16(v[8 * p + 2], v[8 * p + 3]),
                                                                     pack_bf16(v[8 * p + 4], v[8 * p + 5]), pack_bf16(v[8 * p + 6], v[8 * p + 7])));
                     }
                     out.end([&]() {
-                        if (v_row0 < a.V) tma_store_2d(&map_gw, b.c0 + c0, v_row0, patch);
+                        if (v_row0 < a.V) tma_store_2d(&map_gw, b.c0 + c0, v_row0, out.patch);
                     });
                 }
             }

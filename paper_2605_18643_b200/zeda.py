@@ -140,16 +140,16 @@ def _check(status: int):
 
 
 def _ptr(t: Optional[torch.Tensor]):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()  # every pointer argument is declared c_void_p
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # 0.1 us; a torch.cuda.Stream object takes 2.4
 
 
-def _stream(device) -> ctypes.c_void_p:
+def _stream(device) -> int:
     if _raw_stream is None or device.index is None:
-        return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
-    return ctypes.c_void_p(_raw_stream(device.index))
+        return torch.cuda.current_stream(device).cuda_stream
+    return _raw_stream(device.index)
 
 
 def workspace_bytes(cfg: Config) -> int:

@@ -165,6 +165,35 @@ def test_tokens_without_loss_are_left_out():
     m.close()
 
 
+def test_more_tokens_than_the_gathering_threads_take_at_once():
+    # shares of more than 256 tokens per thread block; most carry no loss
+    from paper_2605_18643_b200 import zeda
+    x, w, target, grad = make(160001, 64, 100, seed=21, ignored=0.98)
+    m = zeda.VocabLoss(w, 160001)
+    check(zeda, m, x, w, target, grad)
+    m.close()
+
+
+@pytest.mark.parametrize("d", [512, 576, 2048])
+def test_the_largest_logits_keep_their_digits(d):
+    # hidden states that lean far towards one row of the matrix, which is not the target: the likelihood is that row's logit,
+    # up to 60, less the target's
+    from paper_2605_18643_b200 import zeda
+    for T in (40, 200, 3000):
+        x, w, target, _ = make(T, d, 5000, seed=T + d, lean=1.4)
+        other = ((target.long() + 17) % 5000).to(torch.int32)
+        m = zeda.VocabLoss(w, T, backward=False)
+        nll, lse = m.nll(x, other)
+        r = reference(x, w, other, torch.ones(T, device=DEV))
+        for got, want in ((nll, r[0]), (lse, r[1])):
+            assert bool(((got.double() - want).abs() <= r[2]).all())
+            # logits in 64-bit sums, one rounding of the result and of the references in units of ln 2 (2^-24 of up to 90 each);
+            # at d 512 the tensor cores' sums of 32 additions
+            rms = float((got.double() - want).norm() / want.norm())
+            assert rms <= (3e-7 if d > 512 else 3e-6)
+        m.close()
+
+
 def test_certain_and_impossible_targets():
     from paper_2605_18643_b200 import zeda
     T, d, V = 64, 256, 900

@@ -17,8 +17,10 @@
 //   gradients  by pieces of the vocabulary: X W^T once more, whose epilogue writes the piece's dl as bf16, then in one
 //              launch dl W (added up in fp32 over the pieces) and dl^T X, whose operands lie with the reduction axis
 //              outermost in memory and are read in that layout (MN-major)
-// dl is rounded to bf16 because the tensor cores take both operands in one type and W and X are bf16: 2^-9 relative per
-// term, independent from term to term, so a gradient's error grows to about sqrt(2) times that of its own rounding.
+// dl is rounded to bf16 because the tensor cores take both operands in one type and W and X are bf16: up to 2^-8 relative per
+// term, independent from term to term, so a gradient's error grows to about sqrt(2) times that of its own rounding.  Where
+// few terms make a sum it need not average out, and is mended: what the rounding takes from the target's term is added to
+// grad_x in fp32, and with few tokens what it takes from every term is a second bf16 number, multiplied into grad_w too.
 // Everything else is held in fp32.  No sum's order depends on anything but the sizes.
 #include <cstdlib>
 #include <cstring>
@@ -99,6 +101,7 @@ struct GemmArgs {
     int splits;      // slices of the piece that grad_x is summed in
     int dx_pitch;    // rows between two slices' sums
     int first;       // first piece: the sums start here
+    int rest_row;    // row of dl from which the second numbers lie, 0: there are none
     int back;        // blocks of the logits from the last to the first: the matrix's end is what the pass in front left in L2
     int32_t *meta;
     const int32_t *row_target;
@@ -210,7 +213,7 @@ __device__ __forceinline__ Block block_at(const GemmArgs &a, const Plan &p, int 
         b.m = j / p.dt;
         b.n = j % p.dt;
         b.k0 = 0;
-        b.ks = (p.n_live + kBlockK - 1) / kBlockK;
+        b.ks = (p.n_live + kBlockK - 1) / kBlockK * (a.rest_row ? 2 : 1);
     }
     p.place_columns(b);
     return b;
@@ -477,6 +480,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
             const bool token_rows = !SWAP && (MODE != kModeGrads || b.slice >= 0);
             auto rows_of = [&](int r) { return token_rows ? min(max((plan.n_live - b.m * kTile - 128 * r + 31) / 32 * 32, 32), 128) : 128; };
             const int a_rows = rows_of((int)rank);
+            const int once = (plan.n_live + kBlockK - 1) / kBlockK;  // grad_w: steps over the tokens, then once more with the second numbers
             // the reduction axis innermost: 32 rows a time at least; outermost: boxes of 64 columns
             const uint32_t bytes = (uint32_t)(rows_of(0) + rows_of(1)) * kBlockK * 2 + 2 * ((MODE != kModeGrads ? half * kBlockK * 2 : (half + 63) / 64 * (64 * kBlockK * 2)));
             for (int k = b.k0; k < b.k0 + b.ks; ++k) {
@@ -489,12 +493,12 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                         if (leader) mbar_expect_tx(bar_full + 8 * s, bytes);  // both operands, both CTAs
                         if (SWAP) tma_load_2d_pair(dst, &maps.w_k[0], k * kBlockK, a.v0 + b.m * kTile + 128 * (int)rank, full);
                         else if (token_rows) load_rows(MODE != kModeGrads ? maps.x_k : maps.g_k, dst, k * kBlockK, b.m * kTile + 128 * (int)rank, a_rows, full);
-                        else tma_load_3d_pair(dst, &maps.g_mn, 0, k * kBlockK, 4 * b.m + 2 * (int)rank, full);
+                        else tma_load_3d_pair(dst, &maps.g_mn, 0, k >= once ? a.rest_row + (k - once) * kBlockK : k * kBlockK, 4 * b.m + 2 * (int)rank, full);
                     } else if (MODE != kModeGrads) {
                         load_rows(SWAP ? maps.x_k : maps.w_k, dst, k * kBlockK, (SWAP ? 0 : a.v0) + b0, half, full);
                     } else {
                         const CUtensorMap *m = b.slice >= 0 ? &maps.w_mn : &maps.x_mn;
-                        const int k_at = (b.slice >= 0 ? a.v0 : 0) + k * kBlockK;
+                        const int k_at = b.slice >= 0 ? a.v0 + k * kBlockK : (k >= once ? k - once : k) * kBlockK;
                         tma_load_2d_pair(dst, m, b0, k_at, full);
                         if (half > 64) tma_load_2d_pair(dst + 64 * kBlockK * 2, m, b0 + 64, k_at, full);
                     }
@@ -685,17 +689,29 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                             for (int j = 0; j < 32; ++j)
                                 if (vw + j >= a.V) v[j] = 0.f;
                         }
-                        // 32 tokens x 64 bytes, two patches in turn
-                        const uint32_t patch = out.patch + half_patch * (kStoreBytes / 2);
-                        half_patch ^= 1u;
-                        if (lane == 0) bulk_wait_read<1>();
-                        __syncwarp();
+                        // 32 tokens x 64 bytes, two patches in turn: the numbers, then what their rounding took
 #pragma unroll
-                        for (int p = 0; p < 4; ++p)
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(patch + lane * 64 + ((p ^ ((lane >> 1) & 3)) << 4)),
-                                         "r"(pack_bf16(v[8 * p], v[8 * p + 1])), "r"(pack_bf16(v[8 * p + 2], v[8 * p + 3])),
-                                         "r"(pack_bf16(v[8 * p + 4], v[8 * p + 5])), "r"(pack_bf16(v[8 * p + 6], v[8 * p + 7])) : "memory");
-                        out.end([&]() { tma_store_2d(&maps.g_store_32, vw - a.v0, b.c0 + c0, patch); });
+                        for (int part = 0; part < 2; ++part) {
+                            if (part == 1 && !a.rest_row) break;
+                            const uint32_t patch = out.patch + half_patch * (kStoreBytes / 2);
+                            half_patch ^= 1u;
+                            if (lane == 0) bulk_wait_read<1>();
+                            __syncwarp();
+                            uint32_t packed[16];
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) packed[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+#pragma unroll
+                            for (int p = 0; p < 4; ++p)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(patch + lane * 64 + ((p ^ ((lane >> 1) & 3)) << 4)),
+                                             "r"(packed[4 * p]), "r"(packed[4 * p + 1]), "r"(packed[4 * p + 2]), "r"(packed[4 * p + 3]) : "memory");
+                            out.end([&]() { tma_store_2d(&maps.g_store_32, vw - a.v0, (part ? a.rest_row : 0) + b.c0 + c0, patch); });
+                            if (part == 0)
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) {
+                                    v[2 * j] -= __uint_as_float(packed[j] << 16);
+                                    v[2 * j + 1] -= __uint_as_float(packed[j] & 0xffff0000u);
+                                }
+                        }
                     }
                 }
                 if (MODE == kModeNll) {  // the four quarters' 32 rows each, of every token
@@ -1119,11 +1135,12 @@ vocab_nll_kernel(const NllArgs a) {
     a.lse[t] = (float)(at + loss);
 }
 
-// grad_x: the slices' sums of a row, rounded, to its token; a warp takes 256 columns
+// grad_x: the slices' sums of a row, with what the target's term lost, rounded, to its token; a warp takes 256 columns
 constexpr int kSliceBatch = 5;  // slices fetched at a time
 __global__ void __launch_bounds__(kRowThreads)
 vocab_grad_x_kernel(const int32_t *__restrict__ meta, const float *__restrict__ dx, int splits, size_t slice_stride, int d,
-                    const int32_t *__restrict__ row_token, __nv_bfloat16 *__restrict__ grad_x) {
+                    const int32_t *__restrict__ row_token, const int32_t *__restrict__ row_target, const float *__restrict__ row_gl,
+                    const __nv_bfloat16 *__restrict__ w, __nv_bfloat16 *__restrict__ grad_x) {
     pdl_launch_dependents();
     pdl_wait();
     const int n_live = __ldcg(meta + kLive);
@@ -1134,6 +1151,8 @@ vocab_grad_x_kernel(const int32_t *__restrict__ meta, const float *__restrict__ 
         if (c >= d) continue;
         const int t = __ldcg(row_token + r);
         const float *src = dx + (size_t)r * d + c;
+        const uint4 wt = __ldcg(reinterpret_cast<const uint4 *>(w + (size_t)__ldcg(row_target + r) * d + c));
+        const float gl = __ldcg(row_gl + r), rest = gl - __bfloat162float(__float2bfloat16_rn(gl));
         float4 lo = __ldcg(reinterpret_cast<const float4 *>(src)), hi = __ldcg(reinterpret_cast<const float4 *>(src) + 1);
         for (int s0 = 1; s0 < splits; s0 += kSliceBatch) {
             float4 l[kSliceBatch], h[kSliceBatch];
@@ -1150,6 +1169,14 @@ vocab_grad_x_kernel(const int32_t *__restrict__ meta, const float *__restrict__ 
                     hi.x += h[i].x; hi.y += h[i].y; hi.z += h[i].z; hi.w += h[i].w;
                 }
         }
+        lo.x = fmaf(rest, __uint_as_float(wt.x << 16), lo.x);
+        lo.y = fmaf(rest, __uint_as_float(wt.x & 0xffff0000u), lo.y);
+        lo.z = fmaf(rest, __uint_as_float(wt.y << 16), lo.z);
+        lo.w = fmaf(rest, __uint_as_float(wt.y & 0xffff0000u), lo.w);
+        hi.x = fmaf(rest, __uint_as_float(wt.z << 16), hi.x);
+        hi.y = fmaf(rest, __uint_as_float(wt.z & 0xffff0000u), hi.y);
+        hi.z = fmaf(rest, __uint_as_float(wt.w << 16), hi.z);
+        hi.w = fmaf(rest, __uint_as_float(wt.w & 0xffff0000u), hi.w);
         *reinterpret_cast<uint4 *>(grad_x + (size_t)t * d + c) =
             make_uint4(pack_bf16(lo.x, lo.y), pack_bf16(lo.z, lo.w), pack_bf16(hi.x, hi.y), pack_bf16(hi.z, hi.w));
     }
@@ -1220,7 +1247,7 @@ size_t vocab_carve(const zeda_vocab_config_t &c, unsigned char *base, zeda_vocab
         v.row_lse2 = (float *)take((size_t)v.rows * 4);
         v.row_g = (float *)take((size_t)v.rows * 4);
         v.row_gl = (float *)take((size_t)v.rows * 4);
-        v.g = (__nv_bfloat16 *)take((size_t)v.rows * v.piece * 2);
+        v.g = (__nv_bfloat16 *)take((size_t)(v.rows + kTile) * v.piece * 2);  // (a row block more for the second numbers)
         v.dx = (float *)take((size_t)v.dx_rows * c.d_model * 4);
     }
     if (h) {
@@ -1255,9 +1282,9 @@ bool build_maps(zeda_vocab *h, VocabMaps *m) {
         ok = ok && map_2d(&m->x_k[i], h->xc, h->rows, d, kBlockK, 128 >> i) && map_2d(&m->w_k[i], h->w, V, d, kBlockK, 128 >> i);
     if (ok && h->cfg.backward) {
         ok = map_2d(&m->x_mn, h->xc, h->rows, d, 64, kBlockK) &&
-             map_2d(&m->w_mn, h->w, V, d, 64, kBlockK) && map_mn(&m->g_mn, h->g, h->rows, h->piece) && map_2d(&m->g_store, h->g, h->rows, h->piece, 64, 32) &&
-             map_2d(&m->g_store_32, h->g, h->rows, h->piece, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
-        for (int i = 0; i < 3; ++i) ok = ok && map_2d(&m->g_k[i], h->g, h->rows, h->piece, kBlockK, 128 >> i);
+             map_2d(&m->w_mn, h->w, V, d, 64, kBlockK) && map_mn(&m->g_mn, h->g, h->rows + kTile, h->piece) && map_2d(&m->g_store, h->g, h->rows + kTile, h->piece, 64, 32) &&
+             map_2d(&m->g_store_32, h->g, h->rows + kTile, h->piece, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+        for (int i = 0; i < 3; ++i) ok = ok && map_2d(&m->g_k[i], h->g, h->rows + kTile, h->piece, kBlockK, 128 >> i);
         const cuuint64_t dims[2] = {d, (cuuint64_t)h->dx_rows}, strides[1] = {d * 4};
         const cuuint32_t box[2] = {32, 32};
         ok = ok && encode_f32_map(&m->dx_store, h->dx, 2, dims, strides, box);
@@ -1471,6 +1498,7 @@ zeda_status_t zeda_vocab_nll_backward(zeda_vocab_t *h, const void *x, const int3
     a.splits = grad_x_splits(T, a.d, V < h->piece ? V : h->piece);
     a.dx_pitch = tiles(T) * kTile;
     a.back = V <= h->piece;
+    a.rest_row = tokens_as_columns(T) && T <= kTile ? kTile : 0;
     for (int v0 = 0; v0 < V; v0 += h->piece) {
         a.v0 = v0;
         a.kp = V - v0 < h->piece ? V - v0 : h->piece;
@@ -1483,7 +1511,7 @@ zeda_status_t zeda_vocab_nll_backward(zeda_vocab_t *h, const void *x, const int3
     int ctas = (int)((warps + kRowThreads / 32 - 1) / (kRowThreads / 32) < most ? (warps + kRowThreads / 32 - 1) / (kRowThreads / 32) : most);
     e = launch_kernel(h->pdl, vocab_grad_x_kernel, dim3(ctas), dim3(kRowThreads), 0, s, (const int32_t *)h->meta,
                       (const float *)h->dx, a.splits, (size_t)a.dx_pitch * a.d, a.d, (const int32_t *)h->row_token,
-                      static_cast<__nv_bfloat16 *>(grad_x));
+                      (const int32_t *)h->row_target, (const float *)h->row_gl, h->w, static_cast<__nv_bfloat16 *>(grad_x));
     if (e != cudaSuccess) return vocab_fail("grad_x launch", e);
     return ZEDA_OK;
 }

@@ -194,6 +194,20 @@ def test_the_largest_logits_keep_their_digits(d):
         m.close()
 
 
+@pytest.mark.parametrize("T", [1, 5, 64, 100, 192])
+def test_few_tokens_gradient_of_the_matrix_is_rounded_once(T):
+    # few terms make each of its sums: what the rounding of a logit's gradient takes must not be missing
+    from paper_2605_18643_b200 import zeda
+    x, w, target, grad = make(T, 1024, 3000, seed=T)
+    m = zeda.VocabLoss(w, T)
+    gw = check(zeda, m, x, w, target, grad)[3]
+    want = reference(x, w, target, grad)[4]
+    # the result's own rounding is uniform in +-2^-8 at most: 2^-8 / sqrt(3) rms; a 50th for the rest (2^-17 of the terms and the
+    # logits' errors)
+    assert float((gw.double() - want).norm()) <= 1.02 * HALF / math.sqrt(3) * float(want.norm())
+    m.close()
+
+
 def test_certain_and_impossible_targets():
     from paper_2605_18643_b200 import zeda
     T, d, V = 64, 256, 900

@@ -886,6 +886,10 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
     }
     tc_fence_before();
     __syncthreads();
+    if (s_abort) {  // copies that were on their way when a role gave up land before the CTA leaves
+        const long long t0 = clock64();
+        while (clock64() - t0 < 400000) __nanosleep(1000);
+    }
     cluster_sync_all();
     if (warp == 1) {
         tc_fence_after();

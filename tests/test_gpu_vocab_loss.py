@@ -322,6 +322,68 @@ def test_many_calls_whose_row_blocks_are_mostly_empty(T):
     m.close()
 
 
+@pytest.mark.parametrize("T", [70, 300])
+def test_a_matrix_of_more_than_2_to_the_31_elements(T):
+    from paper_2605_18643_b200 import zeda
+    d, V = 2048, 1_100_003
+    g = torch.Generator(device=DEV)
+    g.manual_seed(T)
+    w = torch.empty((V, d), dtype=torch.bfloat16, device=DEV)
+    for r0 in range(0, V, 100_000):
+        part = w[r0:r0 + 100_000]
+        part.copy_(torch.randn(part.shape, generator=g, device=DEV) * 0.02)
+    target = torch.randint(V - 20_000, V, (T,), generator=g, device=DEV)
+    x = torch.randn(T, d, generator=g, device=DEV) + 20.0 * torch.rand(T, 1, generator=g, device=DEV) * w[target].float()
+    x, target = x.to(torch.bfloat16), target.to(torch.int32)
+    grad = torch.rand(T, generator=g, device=DEV) / T
+    m = zeda.VocabLoss(w, T)
+    nll, lse = m.nll(x, target)
+    gx, gw = m.backward(x, target, nll, lse, grad)
+    m.check()
+    X = x.double()
+    want_lse = torch.full((T,), -math.inf, dtype=torch.float64, device=DEV)
+    for r0 in range(0, V, 50_000):
+        want_lse = torch.logaddexp(want_lse, torch.logsumexp(X @ w[r0:r0 + 50_000].double().t(), dim=1))
+    at = (X * w[target.long()].double()).sum(dim=1)
+    # as the bounds above: d / 16 + 4 additions of 2^-23 of the products' magnitudes, and the results' own roundings
+    mags = (X.abs() * w[target.long()].double().abs()).sum(dim=1).max()
+    tol = 2 * (d / 16 + 4) * 2.0 ** -23 * float(mags) + 8 * 2.0 ** -23 * float(want_lse.abs().max() + 1)
+    assert bool(((lse.double() - want_lse).abs() <= tol).all()) and bool(((nll.double() - (want_lse - at)).abs() <= tol).all())
+    want_gx = torch.zeros((T, d), dtype=torch.float64, device=DEV)
+    for r0 in range(0, V, 50_000):
+        wd = w[r0:r0 + 50_000].double()
+        dl = torch.exp(X @ wd.t() - want_lse[:, None])
+        here = torch.nonzero((target >= r0) & (target < r0 + 50_000))[:, 0]
+        dl[here, target[here].long() - r0] -= 1
+        dl *= grad.double()[:, None]
+        want_gx += dl @ wd
+        got = gw[r0:r0 + 50_000].double()
+        want = dl.t() @ X
+        assert float((got - want).norm()) <= HALF * float(want.norm()), r0
+    assert float((gx.double() - want_gx).norm()) <= HALF * float(want_gx.norm())
+    m.close()
+
+
+def test_an_expired_wait_is_reported_once():
+    # the error word as a kernel's role that gives up leaves it (the second word of the workspace)
+    from paper_2605_18643_b200 import zeda
+    x, w, target, grad = make(16, 128, 300, seed=14)
+    cfg = zeda.VocabConfig(128, 300, 16, 1, 0, 0)
+    ws = torch.empty(int(zeda.lib.zeda_vocab_workspace_bytes(cfg)), dtype=torch.uint8, device=DEV)
+    m = zeda.VocabLoss(w, 16, workspace=ws)
+    m.check()
+    ws.view(torch.int32)[1] = 31
+    with pytest.raises(zeda.ZedaError) as e:
+        m.check()
+    assert e.value.status == zeda.ERR_TIMEOUT
+    m.check()
+    check(zeda, m, x, w, target, grad)
+    ws.view(torch.int32)[1] = 33
+    with pytest.raises(zeda.ZedaError) as e:
+        m.close()
+    assert e.value.status == zeda.ERR_TIMEOUT
+
+
 def test_refusals():
     from paper_2605_18643_b200 import zeda
     x, w, target, grad = make(16, 128, 300, seed=14)

@@ -445,6 +445,8 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == 1) tmem_alloc_pair(smem_u32(&s_tmem_base), 512);
+    if (warp == 2 && lane < (int)(sizeof(VocabMaps) / sizeof(CUtensorMap)))  // the descriptors on their way before the first copy
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<const CUtensorMap *>(&maps) + lane) : "memory");
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();
@@ -566,10 +568,17 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                         if ((++spins & 63) == 0 && (*abort_flag || clock64() - t0 > kWaitLimitCycles)) { ok = false; break; }
                     }
                     if (ok) {
-                        const int ticket = atomicAdd(a.meta + kNextBlock, 1);
-                        // every cluster draws one number behind the last block: the last of them sets the counter back
-                        if (ticket == plan.n_blocks + ((int)gridDim.x >> 1) - 1) atomicExch(a.meta + kNextBlock, 0);
-                        if (ticket < plan.n_blocks) i = ticket;
+                        // the first block is the cluster's own number (a draw takes most of a microsecond); a cluster that has
+                        // one draws until it is past the last, n_blocks draws in all: the last of them sets the counter back
+                        const int n_clusters = (int)gridDim.x >> 1;
+                        if (seq == 0) {
+                            i = (int)blockIdx.x >> 1;
+                        } else {
+                            const int draw = atomicAdd(a.meta + kNextBlock, 1);
+                            if (draw == plan.n_blocks - 1) atomicExch(a.meta + kNextBlock, 0);
+                            i = draw + n_clusters;
+                        }
+                        if (i >= plan.n_blocks) i = -1;
                         const unsigned long long e = ((unsigned long long)(seq + 1) << 32) | (uint32_t)i;
                         asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(peer + 8 * (seq % kQueue)), "l"(e) : "memory");
                         *reinterpret_cast<volatile unsigned long long *>(&s_queue[seq % kQueue]) = e;

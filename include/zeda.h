@@ -344,7 +344,8 @@ zeda_status_t zeda_moe_clear_error(zeda_moe_t *h, void *stream);
 
 /* ---- Training objective: the token term (Eq. 2; weighted token by token, Eq. 3) -----------------------
  * Negative log likelihood of given tokens under a vocabulary matrix, nll_t = log sum_v exp(<x_t, w_v>) - <x_t, w_target>,
- * and its gradients, without the T x n_vocab logits in memory.  fp32 sums over exact bf16 products. */
+ * and its gradients, without the T x n_vocab logits in memory.  Products of bf16 numbers, exact, summed in fp32; of the
+ * likelihoods the target's logit and the largest other one in 64 bits. */
 typedef struct zeda_vocab zeda_vocab_t; /* opaque; host memory owned by the library */
 
 /* Supported: d_model a multiple of 64 in [64, 8192], 1 <= n_vocab <= 2^24, 1 <= max_tokens <= 2^20. */
@@ -352,8 +353,9 @@ typedef struct {
     int32_t d_model;
     int32_t n_vocab;
     int32_t max_tokens;  /* largest T any call will pass */
-    int32_t backward;    /* 1: zeda_vocab_nll_backward will be called (its workspace: up to 256 MB for the gradient of
-                            a piece of the logits, and 4 bytes per element of x) */
+    int32_t backward;    /* 1: zeda_vocab_nll_backward will be called (its workspace: 256 MB or less for the gradient of
+                            a piece of the logits, up to 500,000 tokens; 4 bytes per element of x).  Either way 2 bytes
+                            per element of x and 8 to 12 bytes per token and 256 vocabulary rows */
     int32_t device;      /* CUDA device ordinal */
     int32_t flags;       /* ZEDA_FLAG_* */
 } zeda_vocab_config_t;

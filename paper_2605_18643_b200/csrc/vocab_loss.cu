@@ -13,7 +13,7 @@
 //              relative to it, without the target's (12 bytes per token and 256 logits, with the maximum's place).
 //              The tensor cores' sums lose about 1e-6 of a logit at d 2048 (each of their additions truncates), which
 //              is 1e-5 and more of the likelihood of a likely target: the target's logit, and the largest of the
-//              others where it matters, are summed once more in fp32 on the CUDA cores
+//              others where it matters, are summed once more on the CUDA cores, in 64 bits
 //   gradients  by pieces of the vocabulary: X W^T once more, whose epilogue writes the piece's dl as bf16, then in one
 //              launch dl W (added up in fp32 over the pieces) and dl^T X, whose operands lie with the reduction axis
 //              outermost in memory and are read in that layout (MN-major)

@@ -82,8 +82,8 @@ def test_one_adaptation_step(gate, T, kind):
     # the layer's inner activations, its output, the hidden states and their gradient are each rounded to bf16 on the way (2^-9 rms
     # at most each), the output's error also through the norm: 8 such roundings
     tol = 8 * 2.0 ** -9
-    assert abs(float(balance) - float(want_balance)) <= 1e-5 * float(want_balance)
-    assert abs(float(loss) - float(want)) <= tol * float(want)
+    assert abs(float(balance) - float(want_balance.detach())) <= 1e-5 * float(want_balance.detach())
+    assert abs(float(loss) - float(want.detach())) <= tol * float(want.detach())
     for got, ref in ((grad.double(), l.grad), (grad_vocab.double(), vd.grad)):
         assert float((got - ref).norm()) <= tol * float(ref.norm())
     assert not grad[~padding].any()

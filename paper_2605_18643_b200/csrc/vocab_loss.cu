@@ -77,6 +77,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr size_t kPieceBytes = (size_t)256 << 20;  // of dl at a time
 constexpr int kSwapStages = 10;                  // at most, of narrow column blocks
 constexpr int kSwapTokens = 576;                 // calls of at most so many tokens may take them as the columns of the logits
+constexpr int kRestTokens = 192;                 // up to so many tokens with loss dl is kept as two bf16 numbers
 constexpr int kMaxClusters = 80;                 // CTA pairs of a launch
 constexpr int kMaxSplits = 16;                   // of the vocabulary axis of grad_x
 
@@ -101,7 +102,6 @@ struct GemmArgs {
     int splits;      // slices of the piece that grad_x is summed in
     int dx_pitch;    // rows between two slices' sums
     int first;       // first piece: the sums start here
-    int rest_row;    // row of dl from which the second numbers lie, 0: there are none
     int back;        // blocks of the logits from the last to the first: the matrix's end is what the pass in front left in L2
     int32_t *meta;
     const int32_t *row_target;
@@ -143,6 +143,7 @@ __host__ __device__ inline int logit_blocks(int kp, int n_rb, int n_clusters) {
 
 struct Plan {  // of one launch
     int n_live, n_rb, n_vt, dt, n_blocks;
+    bool rest;         // few tokens: dl as two bf16 numbers, the second a row block behind the first
     Cut cols, slices;  // columns in units of 64; the piece's reduction steps
     __device__ __forceinline__ void place_columns(Block &b) const {
         b.c0 = 64 * cols.start(b.n);
@@ -154,6 +155,7 @@ struct Plan {  // of one launch
 template <int MODE, bool SWAP>
 __device__ __forceinline__ Plan make_plan(const GemmArgs &a, int n_live, int n_clusters) {
     Plan p;
+    p.rest = MODE != kModeNll && n_live <= kRestTokens;
     if (SWAP) {
         p.n_live = n_live;
         p.dt = 0;
@@ -213,7 +215,7 @@ __device__ __forceinline__ Block block_at(const GemmArgs &a, const Plan &p, int 
         b.m = j / p.dt;
         b.n = j % p.dt;
         b.k0 = 0;
-        b.ks = (p.n_live + kBlockK - 1) / kBlockK * (a.rest_row ? 2 : 1);
+        b.ks = (p.n_live + kBlockK - 1) / kBlockK * (p.rest ? 2 : 1);
     }
     p.place_columns(b);
     return b;
@@ -500,7 +502,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                         if (leader) mbar_expect_tx(bar_full + 8 * s, bytes);  // both operands, both CTAs
                         if (SWAP) tma_load_2d_pair(dst, &maps.w_k[0], k * kBlockK, a.v0 + b.m * kTile + 128 * (int)rank, full);
                         else if (token_rows) load_rows(MODE != kModeGrads ? maps.x_k : maps.g_k, dst, k * kBlockK, b.m * kTile + 128 * (int)rank, a_rows, full);
-                        else tma_load_3d_pair(dst, &maps.g_mn, 0, k >= once ? a.rest_row + (k - once) * kBlockK : k * kBlockK, 4 * b.m + 2 * (int)rank, full);
+                        else tma_load_3d_pair(dst, &maps.g_mn, 0, k >= once ? kTile + (k - once) * kBlockK : k * kBlockK, 4 * b.m + 2 * (int)rank, full);
                     } else if (MODE != kModeGrads) {
                         load_rows(SWAP ? maps.x_k : maps.w_k, dst, k * kBlockK, (SWAP ? 0 : a.v0) + b0, half, full);
                     } else {
@@ -707,7 +709,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                         // 32 tokens x 64 bytes, two patches in turn: the numbers, then what their rounding took
 #pragma unroll
                         for (int part = 0; part < 2; ++part) {
-                            if (part == 1 && !a.rest_row) break;
+                            if (part == 1 && !plan.rest) break;
                             const uint32_t patch = out.patch + half_patch * (kStoreBytes / 2);
                             half_patch ^= 1u;
                             if (lane == 0) bulk_wait_read<1>();
@@ -719,7 +721,7 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                             for (int p = 0; p < 4; ++p)
                                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(patch + lane * 64 + ((p ^ ((lane >> 1) & 3)) << 4)),
                                              "r"(packed[4 * p]), "r"(packed[4 * p + 1]), "r"(packed[4 * p + 2]), "r"(packed[4 * p + 3]) : "memory");
-                            out.end([&]() { tma_store_2d(&maps.g_store_32, vw - a.v0, (part ? a.rest_row : 0) + b.c0 + c0, patch); });
+                            out.end([&]() { tma_store_2d(&maps.g_store_32, vw - a.v0, (part ? kTile : 0) + b.c0 + c0, patch); });
                             if (part == 0)
 #pragma unroll
                                 for (int j = 0; j < 16; ++j) {
@@ -823,12 +825,14 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                 // grad_w reduces over whole steps of 64 tokens: zeros behind the last, and nothing further on
                 if (row - lane >= (plan.n_live + kBlockK - 1) / kBlockK * kBlockK) { release(); continue; }
                 if (64 * turn_of >= b.cols) release();
-                for (int c0 = 64 * turn_of; c0 < b.cols; c0 += 128) {
+                const int parts = plan.rest ? 2 : 1;  // the numbers, then (from TMEM once more) what their rounding took
+#pragma unroll 1
+                for (int c0 = 64 * turn_of, part = 0; c0 < b.cols;) {
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         float v[32];
                         tmem_load(t0 + c0 + 32 * half, v);
-                        if (c0 + 128 >= b.cols && half == 1) release();
+                        if (c0 + 128 >= b.cols && half == 1 && part == parts - 1) release();
                         const int c = c0 + 32 * half;
                         gradients_of_logits(v, live, lse2, g);
                         const unsigned hit = (unsigned)(label - c);
@@ -842,13 +846,18 @@ vocab_gemm_kernel(const __grid_constant__ VocabMaps maps, const __grid_constant_
                             for (int j = 0; j < 32; ++j)
                                 if (v_first + c + j >= a.V) v[j] = 0.f;
                         }
+                        if (part) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
+                        }
                         if (half == 0) out.begin();
 #pragma unroll
                         for (int p = 0; p < 4; ++p)
                             out.put(4 * half + p, make_uint4(pack_bf16(v[8 * p], v[8 * p + 1]), pack_bf16(v[8 * p + 2], v[8 * p + 3]),
-                                                                    pack_bf16(v[8 * p + 4], v[8 * p + 5]), pack_bf16(v[8 * p + 6], v[8 * p + 7])));
+                                                             pack_bf16(v[8 * p + 4], v[8 * p + 5]), pack_bf16(v[8 * p + 6], v[8 * p + 7])));
                     }
-                    out.end([&]() { tma_store_2d(&maps.g_store, b.c0 + c0, b.m * kTile + 128 * (int)rank + 32 * q, out.patch); });
+                    out.end([&]() { tma_store_2d(&maps.g_store, b.c0 + c0, part * kTile + b.m * kTile + 128 * (int)rank + 32 * q, out.patch); });
+                    if (++part == parts) { part = 0; c0 += 128; }
                 }
             } else if (b.slice >= 0) {
                 const int row0 = b.slice * a.dx_pitch + b.m * kTile + 128 * (int)rank + 32 * q;
@@ -1517,7 +1526,6 @@ zeda_status_t zeda_vocab_nll_backward(zeda_vocab_t *h, const void *x, const int3
     a.splits = grad_x_splits(T, a.d, V < h->piece ? V : h->piece);
     a.dx_pitch = tiles(T) * kTile;
     a.back = V <= h->piece;
-    a.rest_row = tokens_as_columns(T) && T <= kTile ? kTile : 0;
     for (int v0 = 0; v0 < V; v0 += h->piece) {
         a.v0 = v0;
         a.kp = V - v0 < h->piece ? V - v0 : h->piece;

@@ -194,11 +194,12 @@ def test_the_largest_logits_keep_their_digits(d):
         m.close()
 
 
-@pytest.mark.parametrize("T", [1, 5, 64, 100, 192])
-def test_few_tokens_gradient_of_the_matrix_is_rounded_once(T):
+@pytest.mark.parametrize("T,ignored", [(1, 0.0), (5, 0.0), (64, 0.0), (100, 0.0), (192, 0.0), (250, 0.5), (299, 0.9), (700, 0.95), (3000, 0.95)])
+def test_few_tokens_gradient_of_the_matrix_is_rounded_once(T, ignored):
     # few terms make each of its sums: what the rounding of a logit's gradient takes must not be missing
     from paper_2605_18643_b200 import zeda
-    x, w, target, grad = make(T, 1024, 3000, seed=T)
+    x, w, target, grad = make(T, 1024, 3000, seed=T, ignored=ignored)
+    assert 0 < int((target >= 0).sum()) <= 192
     m = zeda.VocabLoss(w, T)
     gw = check(zeda, m, x, w, target, grad)[3]
     want = reference(x, w, target, grad)[4]
